@@ -252,6 +252,88 @@ rib_status rib_features_bwd(const rib_gen_params *p, const float *W_h, const flo
                             float *dW_h, float *db_h, float *dW_pq, float *dW_pk,
                             void *workspace, size_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Window attention with a LEARNED relative position bias, the bias that RIB stands in for (paper Sec. 2.2; "RPB" in its
+ * Table 4).  Windows, shift, layouts, scales and conventions are those of rib_window_attn_fwd; for every (window, head):
+ *
+ *     S[i][j] = scale_c * q[i].k[j] + bias[head][offset(i, j)]
+ *     offset(i, j) = (iy(i) - iy(j) + M-1) * (2M-1) + ix(i) - ix(j) + M-1         (query minus key, row-major)
+ *     P = softmax over j of S,   O[i] = sum_j P[i][j] v[j],   LSE[i] = log sum_j exp(S[i][j])
+ *
+ * EXCLUDED PAIRS.  A bias of minus infinity, or any at or below -1e30 (so also the lowest value of a type), excludes the pairs of its
+ * offset: their probability and their gradients are exactly zero.  A row whose pairs are all excluded gives O = 0,
+ * LSE = minus infinity and adds nothing to any gradient.  (An infinity or NaN in q, k, v or d_out spreads over its own
+ * (window, head), excluded pairs too, and through the sum over windows into dbias.)
+ *
+ * rib_params: r must be 0 and flags 0 or RIB_FLAG_FORCE_ROW_MAX (else RIB_ERR_UNSUPPORTED); scale_p is not used.  bf16 tensors
+ * may lie on 2-byte boundaries and have any d of 1..64 and any token_stride; even d >= 8, even strides and 4-byte boundaries are
+ * the fast case.  Everything runs on the matrix cores: bf16 storage with bf16 operands (Q times scale_c and P and dS rounded to
+ * nearest) and fp32 sums, fp32 storage in fp32. */
+
+/* Forward.  bias [heads][(2M-1)^2] fp32 (from rib_rpb_table_fwd, or the caller's own); everything else as rib_window_attn_fwd. */
+rib_status rib_rpb_attn_fwd(const rib_params *p, const void *q, const void *k, const void *v, const float *bias,
+                            void *out, float *lse, void *stream);
+
+/* Bytes of device scratch the backward needs (0 if the parameters are invalid): 8 a (token, head), and the
+ * partial sums of dbias of every 256 (bf16) or 128 (fp32) tokens of a window and head. */
+size_t rib_rpb_attn_bwd_workspace_bytes(const rib_params *p);
+
+/* Backward: the probabilities are made again from q, k, bias and lse,
+ *     delta_i = dO[i].out[i]                        (out as it is stored)
+ *     dS[i][j] = P[i][j] (dO[i].v[j] - delta_i)     dV[j] = sum_i P[i][j] dO[i]
+ *     dQ[i] = scale_c sum_j dS[i][j] k[j]           dK[j] = scale_c sum_i dS[i][j] q[i]
+ *     dbias[head][o] = sum over images, windows and the pairs of offset o of dS
+ * dq, dk, dv [B][H][W][C] (dense, dtype of q) and dbias [heads][(2M-1)^2] fp32 are OVERWRITTEN; dbias may be NULL (a bias that is not
+ * trained), which saves its sums.  No result depends on the order in which workgroups run: results are run-to-run
+ * identical.  `workspace`: as for rib_window_attn_bwd, of rib_rpb_attn_bwd_workspace_bytes(p) bytes. */
+rib_status rib_rpb_attn_bwd(const rib_params *p, const void *q, const void *k, const void *v, const float *bias,
+                            const void *out, const void *d_out, const float *lse, void *dq, void *dk, void *dv, float *dbias,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
+/* The learned table: a value for each head and bucket, and the bucket of every offset. */
+typedef struct rib_rpb_params {
+    int32_t window;   /* M, 1..256 */
+    int32_t heads;    /* 1..65535 */
+    int32_t buckets;  /* 1..2^24 */
+    int32_t dtype;    /* rib_dtype of table and dtable */
+} rib_rpb_params;
+
+/* bias[head][o] = table[head][index[o]] for every offset o; where index[o] is negative or not below `buckets`, and where the
+ * table's value is at or below -1e30, minus infinity: the offset's pairs are excluded.
+ * table [heads][buckets] in `dtype`, index [(2M-1)^2], bias [heads][(2M-1)^2] fp32.  Errors: RIB_ERR_NULL, RIB_ERR_SHAPE (a
+ * size outside the ranges above, a misaligned pointer), RIB_ERR_DTYPE, RIB_ERR_LAUNCH. */
+rib_status rib_rpb_table_fwd(const rib_rpb_params *p, const void *table, const int32_t *index, float *bias, void *stream);
+
+/* dtable[head][b] = sum of dbias[head][o] over the offsets with index[o] == b (zero for a bucket without one); OVERWRITTEN.
+ * dbias is what rib_rpb_attn_bwd returns, possibly summed over layers that share the table.  Sums do not depend on the order of their
+ * terms (run-to-run identical results). */
+rib_status rib_rpb_table_bwd(const rib_rpb_params *p, const float *dbias, const int32_t *index, void *dtable, void *stream);
+
+/* ------------------------------------------------------------------------
+ * 8-bit checkpoints of q, k and v, for training steps that keep them between forward and backward: 33 / 60 of their bytes at d = 30 in
+ * bf16, 33 / 120 in fp32.
+ *
+ * Every row of d values (a token's q, k or v of one head) is kept as codes c of 0..255 under one exponent byte e; they stand for
+ *     x = (c - 128) * 2^(e - 127)
+ * with the smallest e >= 1 for which the row's largest magnitude is at most 127 * 2^(e - 127), values rounded to the nearest code (ties
+ * to even).  A row of zeros has e = 0; a row that holds an infinity or NaN has e = 255 and stands for NaN.  What a checkpoint stands
+ * for is exact in bf16 and in fp32, so that packing it again changes nothing.
+ * The buffer (device memory, 16-byte aligned): for q, k, v in turn codes [B*nW*heads][N][16 * ceil(d / 16)] (the columns past d stand for
+ * zero), units numbered as lse's; then for q, k, v exponent bytes [B*nW*heads][N].
+ *
+ * `p` describes the grids as for rib_window_attn_fwd (r, scales and flags do not matter here); q, k, v have token stride
+ * p->token_stride, also where they are written. */
+size_t rib_checkpoint_bytes(const rib_params *p);               /* 0 if the parameters are invalid */
+rib_status rib_checkpoint_pack(const rib_params *p, const void *q, const void *k, const void *v, void *ckpt, void *stream);
+/* The values a checkpoint stands for, as tensors of p->dtype: for rib_window_attn_bwd and the gated backward, or any other use. */
+rib_status rib_checkpoint_unpack(const rib_params *p, const void *ckpt, void *q, void *k, void *v, void *stream);
+
+/* rib_rpb_attn_bwd with the values that `ckpt` stands for in place of q, k and v (bit for bit what it gives for those as tensors),
+ * read from the checkpoint by the kernels themselves.  out and lse are those of the forward, on the values as they were. */
+rib_status rib_rpb_attn_bwd_ckpt(const rib_params *p, const void *ckpt, const float *bias, const void *out, const void *d_out,
+                                 const float *lse, void *dq, void *dk, void *dv, float *dbias,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char *rib_status_string(rib_status st);
 

@@ -26,7 +26,9 @@ EXPORTS = ("rib_window_attn_fwd", "rib_window_attn_bwd", "rib_window_attn_bwd_wo
            "rib_status_string", "rib_window_attn_kernel_name",
            "rib_features_fwd", "rib_features_bwd", "rib_features_bwd_workspace_bytes",
            "rib_window_attn_gated_fwd", "rib_window_attn_gated_bwd", "rib_window_attn_gated_bwd_workspace_bytes",
-           "rib_window_attn_bwd_static_scratch")
+           "rib_window_attn_bwd_static_scratch",
+           "rib_rpb_attn_fwd", "rib_rpb_attn_bwd", "rib_rpb_attn_bwd_workspace_bytes", "rib_rpb_table_fwd", "rib_rpb_table_bwd",
+           "rib_checkpoint_bytes", "rib_checkpoint_pack", "rib_checkpoint_unpack", "rib_rpb_attn_bwd_ckpt")
 RIB_STATIC_SCRATCH_BYTES = 32 << 20
 
 
@@ -44,6 +46,12 @@ class RibGenParams(ctypes.Structure):
     """Mirror of `rib_gen_params`."""
     _fields_ = [("window", ctypes.c_int32), ("heads", ctypes.c_int32), ("r", ctypes.c_int32),
                 ("L", ctypes.c_int32), ("d_h", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class RibRpbParams(ctypes.Structure):
+    """Mirror of `rib_rpb_params`."""
+    _fields_ = [("window", ctypes.c_int32), ("heads", ctypes.c_int32), ("buckets", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
 
 
 class RibError(RuntimeError):
@@ -91,6 +99,26 @@ def load() -> ctypes.CDLL:
     lib.rib_features_bwd_workspace_bytes.argtypes = [gp]
     lib.rib_features_bwd.restype = ctypes.c_int
     lib.rib_features_bwd.argtypes = [gp] + [vp] * 10 + [vp, ctypes.c_size_t, vp]
+    tp = ctypes.POINTER(RibRpbParams)
+    sz = ctypes.c_size_t
+    lib.rib_rpb_attn_fwd.restype = ctypes.c_int
+    lib.rib_rpb_attn_fwd.argtypes = [pp] + [vp] * 6 + [vp]
+    lib.rib_rpb_attn_bwd_workspace_bytes.restype = sz
+    lib.rib_rpb_attn_bwd_workspace_bytes.argtypes = [pp]
+    lib.rib_rpb_attn_bwd.restype = ctypes.c_int
+    lib.rib_rpb_attn_bwd.argtypes = [pp] + [vp] * 11 + [vp, sz, vp]
+    lib.rib_rpb_attn_bwd_ckpt.restype = ctypes.c_int
+    lib.rib_rpb_attn_bwd_ckpt.argtypes = [pp] + [vp] * 9 + [vp, sz, vp]
+    lib.rib_rpb_table_fwd.restype = ctypes.c_int
+    lib.rib_rpb_table_fwd.argtypes = [tp] + [vp] * 3 + [vp]
+    lib.rib_rpb_table_bwd.restype = ctypes.c_int
+    lib.rib_rpb_table_bwd.argtypes = [tp] + [vp] * 3 + [vp]
+    lib.rib_checkpoint_bytes.restype = sz
+    lib.rib_checkpoint_bytes.argtypes = [pp]
+    lib.rib_checkpoint_pack.restype = ctypes.c_int
+    lib.rib_checkpoint_pack.argtypes = [pp] + [vp] * 4 + [vp]
+    lib.rib_checkpoint_unpack.restype = ctypes.c_int
+    lib.rib_checkpoint_unpack.argtypes = [pp] + [vp] * 4 + [vp]
     _lib = lib
     return lib
 
@@ -260,6 +288,111 @@ def rib_features_bwd(p, W_h, b_h, W_pq, W_pk, df_q, df_k, dW_h, db_h, dW_pq, dW_
                                  workspace_bytes, stream)
     if st != RIB_OK:
         raise RibError(st, "rib_features_bwd")
+
+
+# ---- learned relative position bias, 8-bit checkpoints -------------------------------------
+
+def make_rpb_params(window, heads, buckets, dtype="f32") -> RibRpbParams:
+    if isinstance(dtype, str):
+        dtype = {"f32": RIB_F32, "bf16": RIB_BF16}[dtype]
+    return RibRpbParams(window, heads, buckets, dtype)
+
+
+def _ref(p):
+    return ctypes.byref(p) if p is not None else None
+
+
+def _bytes_of(workspace, workspace_bytes):
+    if workspace_bytes is not None:
+        return int(workspace_bytes)
+    return 0 if workspace is None or isinstance(workspace, int) else workspace.numel() * workspace.element_size()
+
+
+def rib_rpb_table_fwd_status(p, table, index, bias, stream=None) -> int:
+    return load().rib_rpb_table_fwd(_ref(p), _ptr(table), _ptr(index), _ptr(bias), _stream(stream) if stream != 0 else 0)
+
+
+def rib_rpb_table_fwd(p, table, index, bias, stream=None) -> None:
+    st = rib_rpb_table_fwd_status(p, table, index, bias, stream)
+    if st != RIB_OK:
+        raise RibError(st, "rib_rpb_table_fwd")
+
+
+def rib_rpb_table_bwd_status(p, dbias, index, dtable, stream=None) -> int:
+    return load().rib_rpb_table_bwd(_ref(p), _ptr(dbias), _ptr(index), _ptr(dtable), _stream(stream) if stream != 0 else 0)
+
+
+def rib_rpb_table_bwd(p, dbias, index, dtable, stream=None) -> None:
+    st = rib_rpb_table_bwd_status(p, dbias, index, dtable, stream)
+    if st != RIB_OK:
+        raise RibError(st, "rib_rpb_table_bwd")
+
+
+def rib_rpb_attn_fwd_status(p, q, k, v, bias, out, lse=None, stream=None) -> int:
+    return load().rib_rpb_attn_fwd(_ref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(bias), _ptr(out), _ptr(lse),
+                                   _stream(stream) if stream != 0 else 0)
+
+
+def rib_rpb_attn_fwd(p, q, k, v, bias, out, lse=None, stream=None) -> None:
+    st = rib_rpb_attn_fwd_status(p, q, k, v, bias, out, lse, stream)
+    if st != RIB_OK:
+        raise RibError(st, "rib_rpb_attn_fwd")
+
+
+def rib_rpb_attn_bwd_workspace_bytes(p) -> int:
+    return int(load().rib_rpb_attn_bwd_workspace_bytes(_ref(p)))
+
+
+def rib_rpb_attn_bwd_status(p, q, k, v, bias, out, d_out, lse, dq, dk, dv, dbias, workspace, workspace_bytes=None,
+                            stream=None) -> int:
+    return load().rib_rpb_attn_bwd(_ref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(bias), _ptr(out), _ptr(d_out), _ptr(lse),
+                                   _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dbias), _ptr(workspace),
+                                   _bytes_of(workspace, workspace_bytes), _stream(stream) if stream != 0 else 0)
+
+
+def rib_rpb_attn_bwd(p, q, k, v, bias, out, d_out, lse, dq, dk, dv, dbias, workspace, workspace_bytes=None,
+                     stream=None) -> None:
+    st = rib_rpb_attn_bwd_status(p, q, k, v, bias, out, d_out, lse, dq, dk, dv, dbias, workspace, workspace_bytes, stream)
+    if st != RIB_OK:
+        raise RibError(st, "rib_rpb_attn_bwd")
+
+
+def rib_rpb_attn_bwd_ckpt_status(p, ckpt, bias, out, d_out, lse, dq, dk, dv, dbias, workspace, workspace_bytes=None,
+                                 stream=None) -> int:
+    return load().rib_rpb_attn_bwd_ckpt(_ref(p), _ptr(ckpt), _ptr(bias), _ptr(out), _ptr(d_out), _ptr(lse), _ptr(dq),
+                                        _ptr(dk), _ptr(dv), _ptr(dbias), _ptr(workspace),
+                                        _bytes_of(workspace, workspace_bytes), _stream(stream) if stream != 0 else 0)
+
+
+def rib_rpb_attn_bwd_ckpt(p, ckpt, bias, out, d_out, lse, dq, dk, dv, dbias, workspace, workspace_bytes=None,
+                          stream=None) -> None:
+    st = rib_rpb_attn_bwd_ckpt_status(p, ckpt, bias, out, d_out, lse, dq, dk, dv, dbias, workspace, workspace_bytes, stream)
+    if st != RIB_OK:
+        raise RibError(st, "rib_rpb_attn_bwd_ckpt")
+
+
+def rib_checkpoint_bytes(p) -> int:
+    return int(load().rib_checkpoint_bytes(_ref(p)))
+
+
+def rib_checkpoint_pack_status(p, q, k, v, ckpt, stream=None) -> int:
+    return load().rib_checkpoint_pack(_ref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(ckpt), _stream(stream) if stream != 0 else 0)
+
+
+def rib_checkpoint_pack(p, q, k, v, ckpt, stream=None) -> None:
+    st = rib_checkpoint_pack_status(p, q, k, v, ckpt, stream)
+    if st != RIB_OK:
+        raise RibError(st, "rib_checkpoint_pack")
+
+
+def rib_checkpoint_unpack_status(p, ckpt, q, k, v, stream=None) -> int:
+    return load().rib_checkpoint_unpack(_ref(p), _ptr(ckpt), _ptr(q), _ptr(k), _ptr(v), _stream(stream) if stream != 0 else 0)
+
+
+def rib_checkpoint_unpack(p, ckpt, q, k, v, stream=None) -> None:
+    st = rib_checkpoint_unpack_status(p, ckpt, q, k, v, stream)
+    if st != RIB_OK:
+        raise RibError(st, "rib_checkpoint_unpack")
 
 
 # ---- device-memory plumbing for tests, smoke and bench (no arithmetic) --------------------

@@ -43,42 +43,6 @@ void *static_scratch(hipError_t *err)
     return ptr;
 }
 
-// Validate everything that does not involve data pointers and fill Geo.
-rib_status make_geo(const rib_params *p, Geo *g)
-{
-    if (p == nullptr) return RIB_ERR_NULL;
-    if (p->B <= 0 || p->H <= 0 || p->W <= 0 || p->heads <= 0 || p->d <= 0 || p->r < 0 || p->window <= 0)
-        return RIB_ERR_SHAPE;
-    if (p->H % p->window != 0 || p->W % p->window != 0) return RIB_ERR_SHAPE;
-    if (p->shift < 0 || p->shift >= p->window) return RIB_ERR_SHAPE;
-    const int64_t C = (int64_t)p->heads * p->d;
-    if (p->token_stride != 0 && p->token_stride < C) return RIB_ERR_SHAPE;
-    if (!std::isfinite(p->scale_c) || !std::isfinite(p->scale_p)) return RIB_ERR_SHAPE;
-    if (p->dtype != RIB_F32 && p->dtype != RIB_BF16) return RIB_ERR_DTYPE;
-    if ((p->flags & ~(RIB_FLAG_FORCE_ROW_MAX | RIB_FLAG_WIDE | RIB_FLAG_VECTOR_ONLY)) != 0) return RIB_ERR_SHAPE;
-    if (p->d > 64 || p->r > 64 || (int64_t)p->window * p->window > 65536 || C > (1 << 20))
-        return RIB_ERR_UNSUPPORTED;
-    g->B = p->B; g->H = p->H; g->W = p->W;
-    g->heads = p->heads; g->d = p->d; g->r = p->r;
-    g->M = p->window; g->s = p->shift;
-    g->N = p->window * p->window;
-    g->nwx = p->W / p->window; g->nwy = p->H / p->window;
-    g->C = (int)C;
-    g->tstride = p->token_stride != 0 ? p->token_stride : C;
-    g->scale_c = p->scale_c; g->scale_p = p->scale_p;
-    g->units = (int64_t)p->B * g->nwx * g->nwy * p->heads;
-    g->gate = nullptr;
-    g->out_raw = nullptr;
-    g->flags = p->flags;
-    g->inv_m = p->window > 1 ? (uint32_t)((((uint64_t)1 << 32) + p->window - 1) / p->window) : 0xffffffffu;
-    // every kernel indexes workgroups with 32-bit block ids and tokens with int
-    const int64_t blocks = g->units * ((g->N + 63) / 64);
-    if (blocks > 0x7fffffffLL || (int64_t)p->B * p->H * p->W > 0x7fffffffLL ||
-        g->units * g->N > ((int64_t)1 << 34))
-        return RIB_ERR_UNSUPPORTED;
-    return RIB_OK;
-}
-
 // The kernels read and write the tensors in 4-byte pieces (bf16 pairs, fp32 values): every
 // data pointer must be 4-byte aligned (NULL passes; presence is checked separately).
 bool aligned4(std::initializer_list<const void *> ptrs)
@@ -116,9 +80,41 @@ rib_status enqueue_bwd(const Geo &g, int dtype, const void *q, const void *k, co
 }
 
 }  // namespace
-}  // namespace rib
 
-namespace rib {
+rib_status make_geo(const rib_params *p, Geo *g)
+{
+    if (p == nullptr) return RIB_ERR_NULL;
+    if (p->B <= 0 || p->H <= 0 || p->W <= 0 || p->heads <= 0 || p->d <= 0 || p->r < 0 || p->window <= 0)
+        return RIB_ERR_SHAPE;
+    if (p->H % p->window != 0 || p->W % p->window != 0) return RIB_ERR_SHAPE;
+    if (p->shift < 0 || p->shift >= p->window) return RIB_ERR_SHAPE;
+    const int64_t C = (int64_t)p->heads * p->d;
+    if (p->token_stride != 0 && p->token_stride < C) return RIB_ERR_SHAPE;
+    if (!std::isfinite(p->scale_c) || !std::isfinite(p->scale_p)) return RIB_ERR_SHAPE;
+    if (p->dtype != RIB_F32 && p->dtype != RIB_BF16) return RIB_ERR_DTYPE;
+    if ((p->flags & ~(RIB_FLAG_FORCE_ROW_MAX | RIB_FLAG_WIDE | RIB_FLAG_VECTOR_ONLY)) != 0) return RIB_ERR_SHAPE;
+    if (p->d > 64 || p->r > 64 || (int64_t)p->window * p->window > 65536 || C > (1 << 20))
+        return RIB_ERR_UNSUPPORTED;
+    g->B = p->B; g->H = p->H; g->W = p->W;
+    g->heads = p->heads; g->d = p->d; g->r = p->r;
+    g->M = p->window; g->s = p->shift;
+    g->N = p->window * p->window;
+    g->nwx = p->W / p->window; g->nwy = p->H / p->window;
+    g->C = (int)C;
+    g->tstride = p->token_stride != 0 ? p->token_stride : C;
+    g->scale_c = p->scale_c; g->scale_p = p->scale_p;
+    g->units = (int64_t)p->B * g->nwx * g->nwy * p->heads;
+    g->gate = nullptr;
+    g->out_raw = nullptr;
+    g->flags = p->flags;
+    g->inv_m = p->window > 1 ? (uint32_t)((((uint64_t)1 << 32) + p->window - 1) / p->window) : 0xffffffffu;
+    // every kernel indexes workgroups with 32-bit block ids and tokens with int
+    const int64_t blocks = g->units * ((g->N + 63) / 64);
+    if (blocks > 0x7fffffffLL || (int64_t)p->B * p->H * p->W > 0x7fffffffLL ||
+        g->units * g->N > ((int64_t)1 << 34))
+        return RIB_ERR_UNSUPPORTED;
+    return RIB_OK;
+}
 
 hipError_t compute_units(int *cus)
 {

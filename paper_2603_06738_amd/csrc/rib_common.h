@@ -136,6 +136,9 @@ __device__ __forceinline__ TokMap fill_tok_map(const Geo &g, int w, int *lds)
     return m;
 }
 
+// Validates everything that does not involve data pointers and fills Geo.
+rib_status make_geo(const rib_params *p, Geo *g);
+
 // Before a launch of a kernel that uses dynamic LDS: raises the kernel's dynamic-LDS limit to
 // kMaxDynLds on the CURRENT device, once per (kernel, device); a failure is returned and not
 // remembered, so a later call tries again.  If `cus` is given it receives the number of compute

@@ -1,0 +1,824 @@
+// Window attention with a learned relative position bias on the bf16 matrix cores: forward, and the backward pair (dq with
+// the bias's gradient, then dkv).  Operator: include/rib_attn.h; the walk and the bias in LDS: rpb_common.h.
+//
+// A wave owns 64 stationary tokens as MFMA B operands, a workgroup W waves; the other side of the unit streams through LDS in
+// tiles of 64 token rows, two stages in turn.  Scores are 32x32 blocks with the streamed tokens as rows, so a lane owns one
+// stationary token and 16 streamed ones; their bias is the C operand of the score product.  What is packed to bf16 there
+// (P, dS) is the B operand of the product that contracts over the streamed tokens, whose A operand is read transposed from
+// the same rows.  Q carries scale * log2 e, rounded to bf16 once, in all three kernels, so that the backward makes the
+// forward's logits again bit for bit.
+//
+// The backward's -LSE and -delta ride in two more columns of Q's and dO's rows, as bf16 pairs (high and low part), against
+// ones in K's and V's: the products are then S - LSE and dP - delta.
+#pragma once
+
+#include "rpb_common.h"
+
+namespace rib {
+namespace rpb {
+namespace bf {
+
+using namespace rows;
+
+constexpr uint32_t kOnes = 0x3f803f80u;
+constexpr float kNoRow = 1e30f;         // in place of LSE * log2 e where a row has no key: every probability is zero
+
+// LDS image of a tile: X and Y rows, a streamed token's lin().  K: columns of the contracted width.
+template <int KX, int KY>
+struct Img {
+    static constexpr int XS = KX + 8, YS = KY + 8;
+    static constexpr int YR = kTile * XS, LT = YR + kTile * YS;
+    static constexpr int STAGE = LT + 2 * kTile;                // bf16 elements
+    static constexpr int TOTAL = 2 * STAGE + 32;                // (transposed reads of the last row may run over its end)
+};
+
+// ---- rows: request, commit ---------------------------------------------------------------------------------------
+
+struct Rows {
+    const char *base;       // grid: this image's and head's slice; checkpoint: this unit's codes
+    int64_t stride;         // bytes between tokens
+    const uint8_t *exps;    // checkpoint: this unit's exponent bytes
+};
+struct Raw {
+    uint32_t w[4];
+};
+struct __attribute__((packed, aligned(4))) u128a4 {
+    uint32_t x, y, z, w;
+};
+template <int SRC>
+__device__ __forceinline__ int piece_col(int j, int d)
+{
+    if (SRC == kAny) return 8 * j;
+    const int n = SRC == kCkpt ? ckpt_row(d) : d;
+    return 8 * j < n - 8 ? 8 * j : n - 8;
+}
+// Piece j (8 values) of token n, which is pixel `t`.
+template <int SRC>
+__device__ __forceinline__ Raw get_piece(const Rows &s, uint32_t t, int n, int j, int d)
+{
+    Raw r;
+    const int c = piece_col<SRC>(j, d);
+    if constexpr (SRC == kCkpt) {
+        const uint2 w = *(const uint2 *)(s.base + (int64_t)n * s.stride + c);
+        r.w[0] = w.x, r.w[1] = w.y, r.w[2] = s.exps[n], r.w[3] = 0u;
+    } else if constexpr (SRC == kFast) {
+        const u128a4 w = *(const u128a4 *)(s.base + (int64_t)t * s.stride + 2 * c);
+        r.w[0] = w.x, r.w[1] = w.y, r.w[2] = w.z, r.w[3] = w.w;
+    } else {
+        const bf16_t *p = (const bf16_t *)(s.base + (int64_t)t * s.stride);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = c + 2 * i < d ? p[c + 2 * i] : 0u, hi = c + 2 * i + 1 < d ? p[c + 2 * i + 1] : 0u;
+            r.w[i] = lo | hi << 16;
+        }
+    }
+    return r;
+}
+// The bf16 pairs of a piece.  A checkpoint's values are exact in bf16: 7 bits under a power of two.
+template <int SRC>
+__device__ __forceinline__ Raw widen_piece(const Raw &r)
+{
+    if constexpr (SRC != kCkpt) return r;
+    const float s = __uint_as_float(r.w[2] << 23), z = -128.f * s;
+    Raw o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = r.w[i >> 1] >> (16 * (i & 1));
+        o.w[i] = trunc_pack(fmaf((float)(w & 255u), s, z), fmaf((float)((w >> 8) & 255u), s, z));
+    }
+    return o;
+}
+template <int SRC>
+__device__ __forceinline__ void put_piece(bf16_t *row, const Raw &r, int j, int d)
+{
+    const int c = piece_col<SRC>(j, d);
+    if (SRC == kAny && c >= d) return;
+    *(u128a4 *)(row + c) = u128a4{r.w[0], r.w[1], r.w[2], r.w[3]};
+}
+__device__ __forceinline__ Raw scaled(Raw r, float s)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.w[i] = scale_pair(r.w[i], s);
+    return r;
+}
+
+// Token n of the window (clamped to the last one) as a pixel of its image.
+__device__ __forceinline__ uint32_t pixel(const Win &w, int n)
+{
+    const int iy = (int)__umulhi((uint32_t)n, w.inv_m);
+    return (uint32_t)(w.rowb[iy] + w.colo[n - __mul24(iy, w.M)]);
+}
+
+// What a thread moves of a tile: LP lanes a token, P passes of nt lanes.
+template <int LP, int W, int SX, int SY, bool EXT>
+struct Mover {
+    static constexpr int NT = 64 * W, P = (kTile * LP + NT - 1) / NT;
+    Raw x[P], y[P];
+    uint2 e[EXT ? P : 1];
+
+    __device__ __forceinline__ void request(const Geo &g, const Win &win, const Rows &xs, const Rows &ys, const uint2 *ext, int tile)
+    {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int slot = p * NT + threadIdx.x, row = slot / LP, j = slot % LP;
+            const int n0 = tile * kTile + row, n = n0 < g.N ? n0 : g.N - 1;
+            const uint32_t t = SX == kCkpt && SY == kCkpt ? 0u : pixel(win, n);
+            x[p] = get_piece<SX>(xs, t, n, j, g.d);
+            y[p] = get_piece<SY>(ys, t, n, j, g.d);
+            if (EXT) e[p] = ext[n];
+        }
+    }
+    // KX, KY: the images' widths.  ONES: ones in the two last columns of both (dq); EXT: -LSE and -delta there (dkv).
+    template <int KX, int KY, bool ONES, bool ALN>
+    __device__ __forceinline__ void commit(const Geo &g, bf16_t *S, int tile, float scale)
+    {
+        using I = Img<KX, KY>;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int slot = p * NT + threadIdx.x, row = slot / LP, j = slot % LP;
+            const int n = tile * kTile + row;
+            const bool in = ALN || n < g.N;
+            bf16_t *xr = S + row * I::XS, *yr = S + I::YR + row * I::YS;
+            Raw a = widen_piece<SX>(x[p]), b = widen_piece<SY>(y[p]);
+            if (EXT) a = scaled(a, scale);
+            if (!in) b.w[0] = b.w[1] = b.w[2] = b.w[3] = 0u;    // (an infinity in the repeated last token must not meet P = 0)
+            if (ONES && SX == kCkpt && piece_col<SX>(j, g.d) == KX - 8) a.w[3] = kOnes;
+            if (ONES && SY == kCkpt && piece_col<SY>(j, g.d) == KY - 8) b.w[3] = kOnes;
+            put_piece<SX>(xr, a, j, g.d);
+            put_piece<SY>(yr, b, j, g.d);
+            if (EXT && j == 0) {
+                *(uint32_t *)(xr + KX - 2) = in ? e[p].x : pack_bf16(-kNoRow, 0.f);
+                *(uint32_t *)(yr + KY - 2) = in ? e[p].y : 0u;
+            }
+            if (!ALN && j == 0) ((int *)(S + I::LT))[row] = lin(g, in ? n : g.N - 1);
+        }
+    }
+};
+// Columns that no commit writes, once for both stages.  `ones`: in the last two columns of X and Y; `one`: in Y's last column.
+template <int KX, int KY>
+__device__ __forceinline__ void init_cols(const Geo &g, bf16_t *S, bool ones, bool one, int nt)
+{
+    using I = Img<KX, KY>;
+    for (int e = threadIdx.x; e < 2 * kTile; e += nt) {
+        bf16_t *xr = S + (e / kTile) * I::STAGE + (e % kTile) * I::XS, *yr = S + (e / kTile) * I::STAGE + I::YR + (e % kTile) * I::YS;
+        for (int c = g.d; c < KX; ++c) xr[c] = ones && c >= KX - 2 ? 0x3f80 : 0;
+        for (int c = g.d; c < KY; ++c) yr[c] = (ones && c >= KY - 2) || (one && c == KY - 1) ? 0x3f80 : 0;
+    }
+}
+
+// A wave's 64 stationary rows as B operands, through `area` (64 rows of K + 8 columns, the wave's own).
+// f(pass, lane-row, j, raw) may change a piece and gets to write columns of the row.
+template <int K, int LP, int SRC, class Fix>
+__device__ __forceinline__ void stationary_rows(const Geo &g, const Win &win, const Rows &s, int n0, bf16_t *area, bf16x8 (&B)[2][K / 16], Fix fix)
+{
+    constexpr int STR = K + 8, R = 64 / LP;             // rows a pass
+    const int lane = threadIdx.x & 63, l = lane / LP, j = lane % LP;
+    Raw r[LP];
+#pragma unroll
+    for (int p = 0; p < LP; ++p) {
+        const int n = n0 + p * R + l, nc = n < g.N ? n : g.N - 1;
+        r[p] = get_piece<SRC>(s, SRC == kCkpt ? 0u : pixel(win, nc), nc, j, g.d);
+    }
+    {
+        bf16_t *xr = area + lane * STR;
+        for (int c = g.d; c < K; ++c) xr[c] = 0;
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int p = 0; p < LP; ++p) {
+        bf16_t *row = area + (p * R + l) * STR;
+        put_piece<SRC>(row, fix(p, widen_piece<SRC>(r[p])), j, g.d);
+    }
+    __builtin_amdgcn_wave_barrier();
+    fix.columns(area, STR);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int b = 0; b < 2; ++b) read_rows<K / 16>(B[b], area + (b * 32 + (lane & 31)) * STR + 8 * (lane >> 5));
+    __builtin_amdgcn_wave_barrier();
+}
+struct FixNone {
+    __device__ __forceinline__ Raw operator()(int, const Raw &r) const { return r; }
+    __device__ __forceinline__ void columns(bf16_t *, int) const {}
+};
+struct FixScale {
+    float s;
+    __device__ __forceinline__ Raw operator()(int, const Raw &r) const { return scaled(r, s); }
+    __device__ __forceinline__ void columns(bf16_t *, int) const {}
+};
+// The pair `w` of row `lane` in the last two columns.
+template <int K>
+struct FixPair {
+    float s;            // 0: values as they are
+    uint32_t w;
+    __device__ __forceinline__ Raw operator()(int, const Raw &r) const { return s != 0.f ? scaled(r, s) : r; }
+    __device__ __forceinline__ void columns(bf16_t *area, int str) const { *(uint32_t *)(area + (threadIdx.x & 63) * str + K - 2) = w; }
+};
+
+// ---- blocks ------------------------------------------------------------------------------------------------------
+
+// LDS words of a lane's 16 streamed tokens of block `kb` of a tile, relative to the lane's own word (c0 - lin(stationary)).
+// Tokens 8a + 4 hf + 0..3: four neighbours each, unless M is no multiple of 8 (then from the tile's table).
+template <bool ALN>
+struct Words16 {
+    int at[ALN ? 4 : 16];
+    __device__ __forceinline__ int operator()(int i) const { return ALN ? at[i >> 2] + (i & 3) : at[ALN ? 0 : i]; }
+};
+template <bool ALN>
+__device__ __forceinline__ Words16<ALN> words_of(const Geo &g, const int *table, int tile, int kb, int hf)
+{
+    Words16<ALN> w;
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+        if constexpr (ALN) {
+            w.at[a] = lin(g, tile * kTile + kb * 32 + 8 * a) + 4 * hf;      // (all but 4 hf uniform)
+        } else {
+            const int4 t = *(const int4 *)(table + kb * 32 + 8 * a + 4 * hf);
+            w.at[4 * a] = t.x, w.at[4 * a + 1] = t.y, w.at[4 * a + 2] = t.z, w.at[4 * a + 3] = t.w;
+        }
+    }
+    return w;
+}
+template <bool ALN>
+__device__ __forceinline__ f32x16 bias_block(const float *mine, const Words16<ALN> &w)
+{
+    f32x16 c;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) c[i] = mine[w(i)];
+    return c;
+}
+
+// Channels 8 (i / 4) + 4 hf .. + 3 of block `db` of a token's row, times `s`.
+template <int SRC>
+__device__ __forceinline__ void store_row(bf16_t *row, const f32x16 &v, int db, int d, int hf, float s)
+{
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+        const int c = 32 * db + 8 * a + 4 * hf, left = d - c;
+        if (left <= 0) continue;
+        const uint32_t w0 = pack_bf16(v[4 * a] * s, v[4 * a + 1] * s), w1 = pack_bf16(v[4 * a + 2] * s, v[4 * a + 3] * s);
+        if (SRC == kAny) {
+            row[c] = (bf16_t)w0;
+            if (left > 1) row[c + 1] = (bf16_t)(w0 >> 16);
+            if (left > 2) row[c + 2] = (bf16_t)w1;
+            if (left > 3) row[c + 3] = (bf16_t)(w1 >> 16);
+        } else {
+            put8(row + c, dword2{w0, w1}, left < 4);
+        }
+    }
+}
+
+// Where a workgroup works: its unit, its block of stationary tokens, the window's map (in `map`, 2 M ints).
+struct Place {
+    int u, blk, w, hd, b;
+    Win win;
+    int64_t img;        // first pixel of the image
+};
+__device__ __forceinline__ Place place_of(const Geo &g, int nblk, int nt, int *map)
+{
+    Place p;
+    int64_t u;
+    block_coords(nblk, u, p.blk);
+    p.u = (int)u, p.w = p.u / g.heads, p.hd = p.u - p.w * g.heads;
+    p.win = window_of<false>(g, p.w, nt, map, p.b);
+    p.img = (int64_t)p.b * g.H * g.W;
+    return p;
+}
+__device__ __forceinline__ Rows grid_rows(const Geo &g, const Place &p, const void *x, int64_t stride)
+{
+    return Rows{(const char *)x + (p.img * stride + p.hd * g.d) * 2, stride * 2, nullptr};
+}
+// Tensor `which` (0 q, 1 k, 2 v) of a unit in a checkpoint.
+__device__ __forceinline__ Rows ckpt_rows_of(const Geo &g, const Place &p, const uint8_t *c, int which)
+{
+    const int dp = ckpt_row(g.d);
+    const int64_t rows = ckpt_rows(g), first = (int64_t)p.u * g.N + which * rows;
+    return Rows{(const char *)c + first * dp, dp, c + 3 * rows * dp + first};
+}
+
+template <int KX, int KY, int W>
+constexpr size_t stage_bytes()
+{
+    using I = Img<KX, KY>;
+    const size_t tiles = (size_t)I::TOTAL * 2, stat = (size_t)W * 64 * (KX + 8) * 2;
+    return ((tiles > stat ? tiles : stat) + 15) & ~(size_t)15;
+}
+
+// ---- forward -----------------------------------------------------------------------------------------------------
+
+// One walk over the keys.  MAX: with the running maximum of every row.
+template <bool MAX, int KX, int DB, bool SUM, int SRC, bool ALN, int W>
+__device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Place &pl, const Rows &ks, const Rows &vs, bf16_t *S, float *B,
+                                         const bf16x8 (&Q)[2][KX / 16], f32x16 (&O)[2][DB], float (&sum)[2], float (&top)[2], int sy0, int sy1,
+                                         const int (&mylin)[2], bool active)
+{
+    constexpr int LP = KX <= 32 ? 4 : 8, KY = 32 * DB, NT = 64 * W;
+    using I = Img<KX, KY>;
+    const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5;
+    const int ntiles = (g.N + kTile - 1) / kTile;
+    const int tro = tr_lane_offset<I::YS>(lane), ako = col * I::XS + 8 * hf;
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) O[qb][db][i] = 0.f;
+        sum[qb] = 0.f, top[qb] = MAX ? -INFINITY : 0.f;
+    }
+    Mover<LP, W, SRC, SRC, false> mv;
+    mv.request(g, pl.win, ks, vs, nullptr, 0);
+    mv.template commit<KX, KY, false, ALN>(g, S, 0, 1.f);
+    mv.request(g, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
+    for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
+        const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
+        const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
+        stage_bias<-1>(g, bi, ch, pl.hd, kLog2e, B, NT);
+        __syncthreads();
+        for (int tile = t0; tile < t1; ++tile) {
+            const bf16_t *cur = S + (tile & 1) * I::STAGE;
+            if (tile + 1 < ntiles) {
+                mv.template commit<KX, KY, false, ALN>(g, S + ((tile + 1) & 1) * I::STAGE, tile + 1, 1.f);
+                mv.request(g, pl.win, ks, vs, nullptr, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
+            }
+            if (active) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const int key0 = tile * kTile + kb * 32;
+                    if (!ALN && key0 >= g.N) break;
+                    const Words16<ALN> wd = words_of<ALN>(g, (const int *)(cur + I::LT), tile, kb, hf);
+                    bf16x8 Ak[KX / 16], At[DB][2];
+                    read_rows<KX / 16>(Ak, cur + kb * 32 * I::XS + ako);
+#pragma unroll
+                    for (int db = 0; db < DB; ++db)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) At[db][i] = read_tr<I::YS>(cur + I::YR + (kb * 32 + 16 * i) * I::YS, tro, 32 * db);
+#pragma unroll
+                    for (int qb = 0; qb < 2; ++qb) {
+                        f32x16 s = bias_block<ALN>(B + ch.c0 - mylin[qb], wd);
+#pragma unroll
+                        for (int i = 0; i < KX / 16; ++i) s = mfma(Ak[i], Q[qb][i], s);
+                        if (!ALN) mask_rows(s, key0, g.N, hf);
+                        if (MAX) {
+                            float m = s[0];
+#pragma unroll
+                            for (int i = 1; i < 16; ++i) m = fmaxf(m, s[i]);
+                            m = fmaxf(top[qb], fmaxf(m, __shfl_xor(m, 32)));
+                            // (a row of minus infinities so far: any finite stabiliser does)
+                            const float ms = m == -INFINITY ? 0.f : m, alpha = __builtin_amdgcn_exp2f(top[qb] - ms);
+                            top[qb] = m;
+                            sum[qb] *= alpha;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) s[i] -= ms;
+#pragma unroll
+                            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) O[qb][db][i] *= alpha;
+                        }
+                        uint32_t P[8];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) P[i] = pack_bf16(s[2 * i], s[2 * i + 1]);
+                        if (SUM) {
+                            float a = 0.f, b = 0.f;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) a += s[2 * i], b += s[2 * i + 1];
+                            sum[qb] += a + b;
+                        }
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) {
+                            O[qb][db] = mfma(At[db][0], as_bf16x8(P[0], P[1], P[2], P[3]), O[qb][db]);
+                            O[qb][db] = mfma(At[db][1], as_bf16x8(P[4], P[5], P[6], P[7]), O[qb][db]);
+                        }
+                    }
+                }
+            }
+            __syncthreads();
+        }
+    }
+    // the denominator: the last row of O^T is register 15 of the upper lane half
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+        const float mine = SUM ? sum[qb] : O[qb][DB - 1][15], other = __shfl_xor(mine, 32);
+        sum[qb] = SUM ? mine + other : hf ? mine : other;
+    }
+}
+
+template <int KX, int DB, bool SUM, int SRC, bool ALN, int W>
+__global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void fwd_kernel(Geo g, Bias bi, int nblk, int force_max, const bf16_t *__restrict__ q,
+                                                        const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
+                                                        bf16_t *__restrict__ out, float *__restrict__ lse)
+{
+    constexpr int LP = KX <= 32 ? 4 : 8, NT = 64 * W;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    bf16_t *S = (bf16_t *)smem;
+    int *map = (int *)(smem + stage_bytes<KX, 32 * DB, W>());
+    float *B = (float *)(map + 2 * g.M);
+    const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place pl = place_of(g, nblk, NT, map);
+    __syncthreads();
+    const int first = pl.blk * NT, last = first + NT < g.N ? first + NT - 1 : g.N - 1, n0 = first + wave * 64;
+    const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m);
+    const bool active = n0 < g.N;
+    bf16x8 Q[2][KX / 16];
+    stationary_rows<KX, LP, SRC>(g, pl.win, grid_rows(g, pl, q, g.tstride), n0, S + wave * 64 * (KX + 8), Q, FixScale{g.scale_c * kLog2e});
+    int mylin[2];
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+        const int n = n0 + qb * 32 + col;
+        mylin[qb] = lin(g, n < g.N ? n : g.N - 1);
+    }
+    __syncthreads();
+    init_cols<KX, 32 * DB>(g, S, false, !SUM, NT);
+    __syncthreads();
+    const Rows ks = grid_rows(g, pl, k, g.tstride), vs = grid_rows(g, pl, v, g.tstride);
+    f32x16 O[2][DB];
+    float sum[2], top[2];
+    // First without a running maximum: exp2 of a logit is a normal number far beyond what bounded logits need.  A row whose
+    // denominator leaves [2^-60, 2^60] sends the workgroup on a second walk, with one.
+    bool bad = true;
+    if (!force_max) {
+        fwd_walk<false, KX, DB, SUM, SRC, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, sy0, sy1, mylin, active);
+        bad = false;
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb)
+            if (active && !((sum[qb] >= 0x1p-60f) && (sum[qb] <= 0x1p60f))) bad = true;
+    }
+    if (__syncthreads_or(bad)) fwd_walk<true, KX, DB, SUM, SRC, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, sy0, sy1, mylin, active);
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+        const int n = n0 + qb * 32 + col;
+        if (n >= g.N) continue;
+        const float inv = sum[qb] == 0.f ? 0.f : 1.f / sum[qb];         // (a row without a key: zeros)
+        if (lse != nullptr && hf == 0)
+            lse[(int64_t)pl.u * g.N + n] = sum[qb] == 0.f ? -INFINITY : (top[qb] + __builtin_amdgcn_logf(sum[qb])) * kLn2;
+        bf16_t *row = out + (pl.img + pixel(pl.win, n)) * g.C + pl.hd * g.d;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) store_row<SRC>(row, O[qb][db], db, g.d, hf, inv);
+    }
+}
+
+// ---- backward: dq and the bias's gradient -------------------------------------------------------------------------
+
+template <int K, int DB, int SRC, int SG, bool ALN, int W, bool HIST>
+__global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias bi, int nblk, int prows, const bf16_t *__restrict__ q,
+                                                       const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
+                                                       const uint8_t *__restrict__ ckpt, const bf16_t *__restrict__ out,
+                                                       const bf16_t *__restrict__ dout, const float *__restrict__ lse,
+                                                       bf16_t *__restrict__ dq, uint2 *__restrict__ ext, float *__restrict__ part)
+{
+    constexpr int LP = DB == 1 ? 4 : 8, NT = 64 * W;
+    using I = Img<K, K>;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    bf16_t *S = (bf16_t *)smem;
+    int *map = (int *)(smem + stage_bytes<K, K, W>());
+    float *B = (float *)(map + 2 * g.M);
+    double *H = (double *)(B + ((bi.rows * bi.w2 + 1) & ~1));           // [wave][hrows * w2]
+    const int hsize = bi.hrows * bi.w2;
+    const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place pl = place_of(g, nblk, NT, map);
+    if (HIST)
+        for (int e = threadIdx.x; e < W * hsize; e += NT) H[e] = 0.;
+    __syncthreads();
+    const int first = pl.blk * NT, last = first + NT < g.N ? first + NT - 1 : g.N - 1, n0 = first + wave * 64;
+    const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m);
+    const bool active = n0 < g.N;
+    bf16x8 Q[2][K / 16], D[2][K / 16];
+    {
+        // delta of the wave's rows: LP lanes share one
+        const Rows os = grid_rows(g, pl, out, g.C), ds = grid_rows(g, pl, dout, g.C);
+        const int l = lane / LP, j = lane % LP, c = piece_col<SG>(j, g.d);
+        float dl[LP];
+#pragma unroll
+        for (int p = 0; p < LP; ++p) {
+            const int n = n0 + p * (64 / LP) + l, nc = n < g.N ? n : g.N - 1;
+            const uint32_t t = pixel(pl.win, nc);
+            const Raw a = get_piece<SG>(os, t, nc, j, g.d), b = get_piece<SG>(ds, t, nc, j, g.d);
+            float s = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {       // (a piece that slid back holds a neighbour's values first)
+                const float x = e & 1 ? hi_bf16(a.w[e >> 1]) * hi_bf16(b.w[e >> 1]) : lo_bf16(a.w[e >> 1]) * lo_bf16(b.w[e >> 1]);
+                s += SG == kAny || c + e >= 8 * j ? x : 0.f;
+            }
+#pragma unroll
+            for (int m = 1; m < LP; m <<= 1) s += __shfl_xor(s, m);
+            dl[p] = s;
+        }
+        // row `lane` belongs to pass lane / (64 / LP), lanes (lane % (64 / LP)) * LP ..
+        float delta = 0.f;
+#pragma unroll
+        for (int p = 0; p < LP; ++p) {
+            const float x = __shfl(dl[p], (lane % (64 / LP)) * LP);
+            if (lane / (64 / LP) == p) delta = x;
+        }
+        const int n = n0 + lane, nc = n < g.N ? n : g.N - 1;
+        const float e = lse[(int64_t)pl.u * g.N + nc];
+        const float L = n >= g.N || e == -INFINITY ? kNoRow : e * kLog2e;
+        const uint32_t wl = L == kNoRow ? pack_bf16(-kNoRow, 0.f) : split_bf16(-L), wd = split_bf16(-delta);
+        if (n < g.N) ext[(int64_t)pl.u * g.N + n] = uint2{wl, wd};
+        bf16_t *area = S + wave * 64 * (K + 8);
+        const Rows qs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 0) : grid_rows(g, pl, q, g.tstride);
+        stationary_rows<K, LP, SRC>(g, pl.win, qs, n0, area, Q, FixPair<K>{g.scale_c * kLog2e, wl});
+        stationary_rows<K, LP, SG>(g, pl.win, ds, n0, area, D, FixPair<K>{0.f, wd});
+    }
+    int mylin[2];
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+        const int n = n0 + qb * 32 + col;
+        mylin[qb] = lin(g, n < g.N ? n : g.N - 1);
+    }
+    // (the wave's own last window row, for its histogram)
+    const int wsy1 = row_of(n0 + 63 < g.N ? n0 + 63 : g.N - 1, g.inv_m);
+    __syncthreads();
+    init_cols<K, K>(g, S, true, false, NT);
+    __syncthreads();
+    const Rows ks = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 1) : grid_rows(g, pl, k, g.tstride);
+    const Rows vs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 2) : grid_rows(g, pl, v, g.tstride);
+    f32x16 A[2][DB];
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) A[qb][db][i] = 0.f;
+    const int ntiles = (g.N + kTile - 1) / kTile;
+    const int tro = tr_lane_offset<I::XS>(lane), ako = col * I::XS + 8 * hf;
+    const f32x16 z = {0};
+    Mover<LP, W, SRC, SRC, false> mv;
+    mv.request(g, pl.win, ks, vs, nullptr, 0);
+    mv.template commit<K, K, true, ALN>(g, S, 0, 1.f);
+    mv.request(g, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
+    int before = -1;            // last streamed row of the chunk before
+    for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
+        const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
+        const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
+        stage_bias<-1>(g, bi, ch, pl.hd, kLog2e, B, NT);
+        double *const mine = H + wave * hsize + ch.c0 - (sy1 - wsy1) * bi.w2;
+        __syncthreads();
+        for (int tile = t0; tile < t1; ++tile) {
+            const bf16_t *cur = S + (tile & 1) * I::STAGE;
+            if (tile + 1 < ntiles) {
+                mv.template commit<K, K, true, ALN>(g, S + ((tile + 1) & 1) * I::STAGE, tile + 1, 1.f);
+                mv.request(g, pl.win, ks, vs, nullptr, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
+            }
+            if (active) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const int key0 = tile * kTile + kb * 32;
+                    if (!ALN && key0 >= g.N) break;
+                    const Words16<ALN> wd = words_of<ALN>(g, (const int *)(cur + I::LT), tile, kb, hf);
+                    bf16x8 Ak[K / 16], Av[K / 16], At[DB][2];
+                    read_rows<K / 16>(Ak, cur + kb * 32 * I::XS + ako);
+                    read_rows<K / 16>(Av, cur + I::YR + kb * 32 * I::YS + ako);
+#pragma unroll
+                    for (int db = 0; db < DB; ++db)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) At[db][i] = read_tr<I::XS>(cur + (kb * 32 + 16 * i) * I::XS, tro, 32 * db);
+#pragma unroll
+                    for (int qb = 0; qb < 2; ++qb) {
+                        f32x16 s = bias_block<ALN>(B + ch.c0 - mylin[qb], wd), p = z;
+#pragma unroll
+                        for (int i = 0; i < K / 16; ++i) s = mfma(Ak[i], Q[qb][i], s);
+#pragma unroll
+                        for (int i = 0; i < K / 16; ++i) p = mfma(Av[i], D[qb][i], p);
+                        if (!ALN) mask_rows(s, key0, g.N, hf);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]) * p[i];
+                        if (HIST) {
+                            double *const h = mine - mylin[qb];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                __hip_atomic_fetch_add(h + wd(i), (double)s[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                        }
+                        uint32_t P[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) P[i] = pack_bf16(s[2 * i], s[2 * i + 1]);
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) {
+                            A[qb][db] = mfma(At[db][0], as_bf16x8(P[0], P[1], P[2], P[3]), A[qb][db]);
+                            A[qb][db] = mfma(At[db][1], as_bf16x8(P[4], P[5], P[6], P[7]), A[qb][db]);
+                        }
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        if (HIST) {
+            flush<W, 64>(g, bi, ch, H, hsize, first, sy0, sy1, before,
+                         part + ((int64_t)pl.u * nblk + pl.blk) * prows * bi.w2 + ch.ty0 * bi.w2);
+            before = ch.ty1;
+        }
+    }
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+        const int n = n0 + qb * 32 + col;
+        if (n >= g.N) continue;
+        bf16_t *row = dq + (pl.img + pixel(pl.win, n)) * g.C + pl.hd * g.d;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) store_row<SG>(row, A[qb][db], db, g.d, hf, g.scale_c);
+    }
+}
+
+// ---- backward: dk, dv --------------------------------------------------------------------------------------------
+
+template <int K, int DB, int SRC, int SG, bool ALN, int W>
+__global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias bi, int nblk, const bf16_t *__restrict__ q,
+                                                        const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
+                                                        const uint8_t *__restrict__ ckpt, const bf16_t *__restrict__ dout,
+                                                        const uint2 *__restrict__ ext, bf16_t *__restrict__ dk, bf16_t *__restrict__ dv)
+{
+    constexpr int LP = DB == 1 ? 4 : 8, NT = 64 * W;
+    using I = Img<K, K>;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    bf16_t *S = (bf16_t *)smem;
+    int *map = (int *)(smem + stage_bytes<K, K, W>());
+    float *B = (float *)(map + 2 * g.M);
+    const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place pl = place_of(g, nblk, NT, map);
+    __syncthreads();
+    const int first = pl.blk * NT, last = first + NT < g.N ? first + NT - 1 : g.N - 1, n0 = first + wave * 64;
+    const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m);
+    const bool active = n0 < g.N;
+    bf16x8 Kb[2][K / 16], Vb[2][K / 16];
+    {
+        bf16_t *area = S + wave * 64 * (K + 8);
+        const Rows ks = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 1) : grid_rows(g, pl, k, g.tstride);
+        const Rows vs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 2) : grid_rows(g, pl, v, g.tstride);
+        stationary_rows<K, LP, SRC>(g, pl.win, ks, n0, area, Kb, FixPair<K>{0.f, kOnes});
+        stationary_rows<K, LP, SRC>(g, pl.win, vs, n0, area, Vb, FixPair<K>{0.f, kOnes});
+    }
+    int mylin[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        const int n = n0 + b * 32 + col;
+        mylin[b] = lin(g, n < g.N ? n : g.N - 1);
+    }
+    __syncthreads();
+    init_cols<K, K>(g, S, false, false, NT);
+    __syncthreads();
+    const Rows qs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 0) : grid_rows(g, pl, q, g.tstride), ds = grid_rows(g, pl, dout, g.C);
+    const uint2 *const ex = ext + (int64_t)pl.u * g.N;
+    f32x16 Ak[2][DB], Av[2][DB];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) Ak[b][db][i] = 0.f, Av[b][db][i] = 0.f;
+    const int ntiles = (g.N + kTile - 1) / kTile;
+    const int tro = tr_lane_offset<I::XS>(lane), ako = col * I::XS + 8 * hf;
+    const float scale = g.scale_c * kLog2e;
+    const f32x16 z = {0};
+    Mover<LP, W, SRC, SG, true> mv;
+    mv.request(g, pl.win, qs, ds, ex, 0);
+    mv.template commit<K, K, false, ALN>(g, S, 0, scale);
+    mv.request(g, pl.win, qs, ds, ex, ntiles > 1 ? 1 : 0);
+    for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
+        const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
+        const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
+        stage_bias<1>(g, bi, ch, pl.hd, kLog2e, B, NT);
+        __syncthreads();
+        for (int tile = t0; tile < t1; ++tile) {
+            const bf16_t *cur = S + (tile & 1) * I::STAGE;
+            if (tile + 1 < ntiles) {
+                mv.template commit<K, K, false, ALN>(g, S + ((tile + 1) & 1) * I::STAGE, tile + 1, scale);
+                mv.request(g, pl.win, qs, ds, ex, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
+            }
+            if (active) {
+#pragma unroll
+                for (int qb = 0; qb < 2; ++qb) {
+                    if (!ALN && tile * kTile + qb * 32 >= g.N) break;
+                    const Words16<ALN> wd = words_of<ALN>(g, (const int *)(cur + I::LT), tile, qb, hf);
+                    bf16x8 Aq[K / 16], Ad[K / 16], Tq[DB][2], Td[DB][2];
+                    read_rows<K / 16>(Aq, cur + qb * 32 * I::XS + ako);
+                    read_rows<K / 16>(Ad, cur + I::YR + qb * 32 * I::YS + ako);
+#pragma unroll
+                    for (int db = 0; db < DB; ++db)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            Tq[db][i] = read_tr<I::XS>(cur + (qb * 32 + 16 * i) * I::XS, tro, 32 * db);
+                            Td[db][i] = read_tr<I::YS>(cur + I::YR + (qb * 32 + 16 * i) * I::YS, tro, 32 * db);
+                        }
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        f32x16 s = bias_block<ALN>(B + ch.c0 - mylin[b], wd), p = z;
+#pragma unroll
+                        for (int i = 0; i < K / 16; ++i) s = mfma(Aq[i], Kb[b][i], s);
+#pragma unroll
+                        for (int i = 0; i < K / 16; ++i) p = mfma(Ad[i], Vb[b][i], p);
+                        uint32_t P[8], G[8];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            P[i] = pack_bf16(s[2 * i], s[2 * i + 1]);
+                            G[i] = pack_bf16(s[2 * i] * p[2 * i], s[2 * i + 1] * p[2 * i + 1]);
+                        }
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) {
+                            Av[b][db] = mfma(Td[db][0], as_bf16x8(P[0], P[1], P[2], P[3]), Av[b][db]);
+                            Av[b][db] = mfma(Td[db][1], as_bf16x8(P[4], P[5], P[6], P[7]), Av[b][db]);
+                            Ak[b][db] = mfma(Tq[db][0], as_bf16x8(G[0], G[1], G[2], G[3]), Ak[b][db]);
+                            Ak[b][db] = mfma(Tq[db][1], as_bf16x8(G[4], G[5], G[6], G[7]), Ak[b][db]);
+                        }
+                    }
+                }
+            }
+            __syncthreads();
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        const int n = n0 + b * 32 + col;
+        if (n >= g.N) continue;
+        const int64_t at = (pl.img + pixel(pl.win, n)) * g.C + pl.hd * g.d;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+            store_row<SG>(dk + at, Ak[b][db], db, g.d, hf, kLn2);       // (Q carries scale * log2 e)
+            store_row<SG>(dv + at, Av[b][db], db, g.d, hf, 1.f);
+        }
+    }
+}
+
+// ---- launches ----------------------------------------------------------------------------------------------------
+
+constexpr size_t kBiasBytes = 36 * 1024, kHistBytes = 9 * 1024;
+
+template <int KX, int DB, bool SUM, int SRC, bool ALN, int W>
+hipError_t launch_fwd_one(const Geo &g, const FwdArgs &a)
+{
+    Bias bi{a.bias, 0, 0, 0, 0};
+    plan_chunks(g, RIB_BF16, &bi, false, kBiasBytes, 0);
+    const int nblk = (g.N + 64 * W - 1) / (64 * W);
+    const size_t smem = stage_bytes<KX, 32 * DB, W>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.w2 * 4;
+    if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
+    auto kern = fwd_kernel<KX, DB, SUM, SRC, ALN, W>;
+    const hipError_t e = prepare_kernel((const void *)kern, nullptr);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * nblk)), dim3(64 * W), smem, a.st, g, bi, nblk, a.force_max, (const bf16_t *)a.q,
+                       (const bf16_t *)a.k, (const bf16_t *)a.v, (bf16_t *)a.out, a.lse);
+    return hipGetLastError();
+}
+template <int KX, int DB, bool SUM, int SRC>
+hipError_t launch_fwd_src(const Geo &g, const FwdArgs &a)
+{
+    if (g.N <= 64) return launch_fwd_one<KX, DB, SUM, SRC, false, 1>(g, a);
+    if (SRC == kFast && g.M % 8 == 0) return launch_fwd_one<KX, DB, SUM, SRC, SRC == kFast, 4>(g, a);
+    return launch_fwd_one<KX, DB, SUM, SRC, false, 4>(g, a);
+}
+
+template <int K, int DB, int SRC, int SG, bool ALN, int W, bool HIST>
+hipError_t launch_dq_one(const Geo &g, const BwdArgs &a, const Ws &ws)
+{
+    Bias bi{a.bias, 0, 0, 0, 0};
+    plan_chunks(g, RIB_BF16, &bi, HIST, kBiasBytes, kHistBytes);
+    const size_t smem = stage_bytes<K, K, W>() + 8 * (size_t)g.M + ((size_t)bi.rows * bi.w2 + 1) / 2 * 8 + (size_t)W * bi.hrows * bi.w2 * 8;
+    if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
+    auto kern = dq_kernel<K, DB, SRC, SG, ALN, W, HIST>;
+    const hipError_t e = prepare_kernel((const void *)kern, nullptr);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * ws.nblk)), dim3(64 * W), smem, a.st, g, bi, ws.nblk, ws.prows, (const bf16_t *)a.q,
+                       (const bf16_t *)a.k, (const bf16_t *)a.v, a.ckpt, (const bf16_t *)a.out, (const bf16_t *)a.dout, a.lse,
+                       (bf16_t *)a.dq, (uint2 *)((char *)a.ws + ws.ext), (float *)((char *)a.ws + ws.part));
+    return hipGetLastError();
+}
+template <int K, int DB, int SRC, int SG, bool ALN, int W>
+hipError_t launch_pair(const Geo &g, const BwdArgs &a, const Ws &ws)
+{
+    hipError_t e = a.dbias != nullptr ? launch_dq_one<K, DB, SRC, SG, ALN, W, true>(g, a, ws) : launch_dq_one<K, DB, SRC, SG, ALN, W, false>(g, a, ws);
+    if (e != hipSuccess) return e;
+    Bias bi{a.bias, 0, 0, 0, 0};
+    plan_chunks(g, RIB_BF16, &bi, false, kBiasBytes, 0);
+    const size_t smem = stage_bytes<K, K, W>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.w2 * 4;
+    if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
+    auto kern = dkv_kernel<K, DB, SRC, SG, ALN, W>;
+    e = prepare_kernel((const void *)kern, nullptr);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * ws.nblk)), dim3(64 * W), smem, a.st, g, bi, ws.nblk, (const bf16_t *)a.q,
+                       (const bf16_t *)a.k, (const bf16_t *)a.v, a.ckpt, (const bf16_t *)a.dout, (const uint2 *)((const char *)a.ws + ws.ext),
+                       (bf16_t *)a.dk, (bf16_t *)a.dv);
+    return hipGetLastError();
+}
+template <int K, int DB, int SRC, int SG>
+hipError_t launch_bwd_src(const Geo &g, const BwdArgs &a, const Ws &ws)
+{
+    if (g.N <= 64) return launch_pair<K, DB, SRC, SG, false, 1>(g, a, ws);
+    if (SG == kFast && g.M % 8 == 0) return launch_pair<K, DB, SRC, SG, SG == kFast, 4>(g, a, ws);
+    return launch_pair<K, DB, SRC, SG, false, 4>(g, a, ws);
+}
+template <int K, int DB, int SG>
+hipError_t launch_bwd(const Geo &g, const BwdArgs &a, const Ws &ws)
+{
+    return a.ckpt != nullptr ? launch_bwd_src<K, DB, kCkpt, SG>(g, a, ws) : launch_bwd_src<K, DB, SG, SG>(g, a, ws);
+}
+
+// One translation unit a width.
+hipError_t bwd32(const Geo &, const BwdArgs &, const Ws &);
+hipError_t bwd48(const Geo &, const BwdArgs &, const Ws &);
+hipError_t bwd48w(const Geo &, const BwdArgs &, const Ws &);
+hipError_t bwd64(const Geo &, const BwdArgs &, const Ws &);
+hipError_t bwd80(const Geo &, const BwdArgs &, const Ws &);
+hipError_t bwd_any(const Geo &, const BwdArgs &, const Ws &);
+
+}  // namespace bf
+}  // namespace rpb
+}  // namespace rib

@@ -1,0 +1,13 @@
+// Backward pair of the learned relative position bias, bf16: odd or short rows and unaligned tensors.
+#include "rpb_bf16.h"
+
+namespace rib {
+namespace rpb {
+namespace bf {
+hipError_t bwd_any(const Geo &g, const BwdArgs &a, const Ws &ws)
+{
+    return g.d <= 32 ? launch_bwd<48, 1, kAny>(g, a, ws) : launch_bwd<80, 2, kAny>(g, a, ws);
+}
+}  // namespace bf
+}  // namespace rpb
+}  // namespace rib

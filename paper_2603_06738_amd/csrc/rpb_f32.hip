@@ -1,0 +1,527 @@
+// Window attention with a learned relative position bias, fp32 storage, on the fp32 matrix instruction (32x32x2): products,
+// sums and softmax state in fp32.  Operator: include/rib_attn.h; the walk and the bias in LDS: rpb_common.h.
+//
+// A wave owns 32 stationary tokens, a workgroup W waves; the other side streams through LDS in tiles of 64 token rows, two
+// stages in turn.  Scores have the streamed tokens as rows: a lane owns one stationary token and 16 streamed ones, and its
+// P and dS are, register by register, the B operands of the product that contracts over the streamed tokens (k = 0 and 1 of
+// an instruction are the two lane halves).  What bounds it is that instruction: a 32x32 block at 32 channels is 16 of them
+// a product (64 clk each), the exponentials beside it a tenth.
+#include "rpb_bf16.h"
+
+namespace rib {
+namespace rpb {
+namespace fp {
+
+using namespace rows;
+using bf::bias_block;
+using bf::Place;
+using bf::place_of;
+using bf::pixel;
+using bf::Words16;
+using bf::words_of;
+
+__device__ __forceinline__ f32x16 mfma2(float a, float b, const f32x16 &c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
+
+template <int DB>
+struct Img {
+    static constexpr int STR = 32 * DB + 4;                     // floats: an odd number of 16 bytes
+    static constexpr int YR = kTile * STR, LT = 2 * YR, EX = LT + kTile;
+    static constexpr int STAGE = EX + 2 * kTile;
+};
+
+struct Rows {
+    const char *base;
+    int64_t stride;         // bytes between tokens
+    const uint8_t *exps;
+};
+__device__ __forceinline__ Rows rows_of_grid(const Geo &g, const Place &p, const void *x, int64_t stride)
+{
+    return Rows{(const char *)x + (p.img * stride + p.hd * g.d) * 4, stride * 4, nullptr};
+}
+// Values c .. c+3 of a token's row (zeros past the head).  With a checkpoint a raw word of codes and the exponent.
+struct Raw {
+    float x, y, z, w;
+};
+template <bool CKPT>
+__device__ __forceinline__ Raw get4(const Rows &s, uint32_t t, int n, int c, int d)
+{
+    if constexpr (CKPT) {
+        const int dp = ckpt_row(d);
+        const uint32_t w = c < dp ? *(const uint32_t *)(s.base + (int64_t)n * s.stride + c) : 0x80808080u;
+        const float sc = __uint_as_float((uint32_t)s.exps[n] << 23), z = -128.f * sc;
+        return Raw{fmaf((float)(w & 255u), sc, z), fmaf((float)((w >> 8) & 255u), sc, z), fmaf((float)((w >> 16) & 255u), sc, z),
+                   fmaf((float)(w >> 24), sc, z)};
+    } else {
+        const float *p = (const float *)(s.base + (int64_t)t * s.stride) + c;
+        if (c + 4 <= d) {
+            const float4u v = *(const float4u *)p;
+            return Raw{v.x, v.y, v.z, v.w};
+        }
+        return Raw{c < d ? p[0] : 0.f, c + 1 < d ? p[1] : 0.f, c + 2 < d ? p[2] : 0.f, 0.f};
+    }
+}
+
+template <int DB, int W, bool CX, bool CY, bool EXT>
+struct Mover {
+    static constexpr int LP = 8 * DB, NT = 64 * W, P = (kTile * LP + NT - 1) / NT;
+    Raw x[P], y[P];
+    float2 e;
+
+    __device__ __forceinline__ void request(const Geo &g, const Win &win, const Rows &xs, const Rows &ys, const float2 *ext, int tile)
+    {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int slot = p * NT + threadIdx.x, row = slot / LP, j = slot % LP;
+            const int n0 = tile * kTile + row, n = n0 < g.N ? n0 : g.N - 1;
+            const uint32_t t = CX && CY ? 0u : pixel(win, n);
+            x[p] = get4<CX>(xs, t, n, 4 * j, g.d);
+            y[p] = get4<CY>(ys, t, n, 4 * j, g.d);
+        }
+        if (EXT && threadIdx.x < kTile) {
+            const int n = tile * kTile + threadIdx.x;
+            e = n < g.N ? ext[n] : float2{-bf::kNoRow, 0.f};
+        }
+    }
+    __device__ __forceinline__ void commit(const Geo &g, float *S, int tile, float scale)
+    {
+        using I = Img<DB>;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int slot = p * NT + threadIdx.x, row = slot / LP, j = slot % LP;
+            Raw a = x[p], b = y[p];
+            if (EXT) a.x *= scale, a.y *= scale, a.z *= scale, a.w *= scale;
+            if (tile * kTile + row >= g.N) b.x = b.y = b.z = b.w = 0.f;     // (an infinity in the repeated last token must not meet P = 0)
+            *(Raw *)(S + row * I::STR + 4 * j) = a;
+            *(Raw *)(S + I::YR + row * I::STR + 4 * j) = b;
+        }
+        if (threadIdx.x < kTile) {
+            const int n = tile * kTile + threadIdx.x;
+            ((int *)(S + I::LT))[threadIdx.x] = lin(g, n < g.N ? n : g.N - 1);
+            if (EXT) S[I::EX + threadIdx.x] = e.x, S[I::EX + kTile + threadIdx.x] = e.y;
+        }
+    }
+};
+
+// A lane's B operands of its stationary token: channels 8 s + 4 hf .. + 3 of step s.
+template <int DB, bool CKPT>
+__device__ __forceinline__ void operand(const Geo &g, const Place &pl, const Rows &s, int n, float scale, Raw (&B)[4 * DB])
+{
+    const int hf = (threadIdx.x & 63) >> 5;
+    const uint32_t t = CKPT ? 0u : pixel(pl.win, n);
+#pragma unroll
+    for (int k = 0; k < 4 * DB; ++k) {
+        B[k] = get4<CKPT>(s, t, n, 8 * k + 4 * hf, g.d);
+        B[k].x *= scale, B[k].y *= scale, B[k].z *= scale, B[k].w *= scale;
+    }
+}
+// 32 streamed rows against the lane's operands: `row` is this lane's streamed row (+ 4 hf).
+template <int DB>
+__device__ __forceinline__ f32x16 scores(const float *row, const Raw (&B)[4 * DB], f32x16 c, int d)
+{
+#pragma unroll
+    for (int k = 0; k < 4 * DB; ++k) {
+        if (8 * k >= d) break;
+        const Raw a = *(const Raw *)(row + 8 * k);
+        c = mfma2(a.x, B[k].x, c);
+        c = mfma2(a.y, B[k].y, c);
+        c = mfma2(a.z, B[k].z, c);
+        c = mfma2(a.w, B[k].w, c);
+    }
+    return c;
+}
+// acc^T += rows^T p: `col` is the block's first streamed row + 4 hf rows + this lane's channel.
+template <int DB>
+__device__ __forceinline__ void contract(f32x16 (&acc)[DB], const float *col, const f32x16 &p)
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[db] = mfma2(col[(8 * (i >> 2) + (i & 3)) * Img<DB>::STR + 32 * db], p[i], acc[db]);
+}
+template <int DB>
+__device__ __forceinline__ void store_row(float *row, const f32x16 (&v)[DB], int d, int hf, float s)
+{
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const int c = 32 * db + 8 * a + 4 * hf;
+            if (c + 4 <= d) *(float4u *)(row + c) = float4u{v[db][4 * a] * s, v[db][4 * a + 1] * s, v[db][4 * a + 2] * s, v[db][4 * a + 3] * s};
+            else
+#pragma unroll
+                for (int r = 0; r < 3; ++r)
+                    if (c + r < d) row[c + r] = v[db][4 * a + r] * s;
+        }
+}
+template <int DB>
+constexpr size_t stage_bytes()
+{
+    return (size_t)2 * Img<DB>::STAGE * 4;
+}
+__device__ __forceinline__ Rows rows_of_ckpt(const Geo &g, const Place &p, const uint8_t *c, int which)
+{
+    const bf::Rows r = bf::ckpt_rows_of(g, p, c, which);
+    return Rows{r.base, r.stride, r.exps};
+}
+
+template <bool MAX, int DB, bool ALN, int W>
+__device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Place &pl, const Rows &ks, const Rows &vs, float *S, float *B,
+                                         const Raw (&Q)[4 * DB], f32x16 (&O)[DB], float &sum, float &top, int sy0, int sy1, int mylin, bool active)
+{
+    using I = Img<DB>;
+    constexpr int NT = 64 * W;
+    const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5;
+    const int ntiles = (g.N + kTile - 1) / kTile;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) O[db][i] = 0.f;
+    sum = 0.f, top = MAX ? -INFINITY : 0.f;
+    Mover<DB, W, false, false, false> mv;
+    mv.request(g, pl.win, ks, vs, nullptr, 0);
+    mv.commit(g, S, 0, 1.f);
+    mv.request(g, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
+    for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
+        const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
+        const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
+        stage_bias<-1>(g, bi, ch, pl.hd, kLog2e, B, NT);
+        __syncthreads();
+        for (int tile = t0; tile < t1; ++tile) {
+            const float *cur = S + (tile & 1) * I::STAGE;
+            if (tile + 1 < ntiles) {
+                mv.commit(g, S + ((tile + 1) & 1) * I::STAGE, tile + 1, 1.f);
+                mv.request(g, pl.win, ks, vs, nullptr, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
+            }
+            if (active) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const int key0 = tile * kTile + kb * 32;
+                    if (!ALN && key0 >= g.N) break;
+                    const Words16<ALN> wd = words_of<ALN>(g, (const int *)(cur + I::LT), tile, kb, hf);
+                    f32x16 s = scores<DB>(cur + (kb * 32 + col) * I::STR + 4 * hf, Q, bias_block<ALN>(B + ch.c0 - mylin, wd), g.d);
+                    if (!ALN) mask_rows(s, key0, g.N, hf);
+                    if (MAX) {
+                        float m = s[0];
+#pragma unroll
+                        for (int i = 1; i < 16; ++i) m = fmaxf(m, s[i]);
+                        m = fmaxf(top, fmaxf(m, __shfl_xor(m, 32)));
+                        // (a row of minus infinities so far: any finite stabiliser does)
+                        const float ms = m == -INFINITY ? 0.f : m, alpha = __builtin_amdgcn_exp2f(top - ms);
+                        top = m;
+                        sum *= alpha;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] -= ms;
+#pragma unroll
+                        for (int db = 0; db < DB; ++db)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) O[db][i] *= alpha;
+                    }
+                    float a = 0.f, b = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) a += s[2 * i], b += s[2 * i + 1];
+                    sum += a + b;
+                    contract<DB>(O, cur + I::YR + (kb * 32 + 4 * hf) * I::STR + col, s);
+                }
+            }
+            __syncthreads();
+        }
+    }
+    sum += __shfl_xor(sum, 32);
+}
+
+template <int DB, bool ALN, int W>
+__global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void fwd_kernel(Geo g, Bias bi, int nblk, int force_max, const float *__restrict__ q,
+                                                        const float *__restrict__ k, const float *__restrict__ v, float *__restrict__ out,
+                                                        float *__restrict__ lse)
+{
+    constexpr int NT = 64 * W, SB = 32 * W;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    float *S = (float *)smem;
+    int *map = (int *)(smem + stage_bytes<DB>());
+    float *B = (float *)(map + 2 * g.M);
+    const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place pl = place_of(g, nblk, NT, map);
+    __syncthreads();
+    const int first = pl.blk * SB, last = first + SB < g.N ? first + SB - 1 : g.N - 1, n0 = first + wave * 32, n = n0 + col;
+    const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m), nc = n < g.N ? n : g.N - 1;
+    const bool active = n0 < g.N;
+    Raw Q[4 * DB];
+    operand<DB, false>(g, pl, rows_of_grid(g, pl, q, g.tstride), nc, g.scale_c * kLog2e, Q);
+    const Rows ks = rows_of_grid(g, pl, k, g.tstride), vs = rows_of_grid(g, pl, v, g.tstride);
+    f32x16 O[DB];
+    float sum, top;
+    // First without a running maximum; a denominator outside [2^-60, 2^60] sends the workgroup on a second walk, with one.
+    bool bad = true;
+    if (!force_max) {
+        fwd_walk<false, DB, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, sy0, sy1, lin(g, nc), active);
+        bad = active && !((sum >= 0x1p-60f) && (sum <= 0x1p60f));
+    }
+    if (__syncthreads_or(bad)) fwd_walk<true, DB, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, sy0, sy1, lin(g, nc), active);
+    if (n >= g.N) return;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;         // (a row without a key: zeros)
+    if (lse != nullptr && hf == 0) lse[(int64_t)pl.u * g.N + n] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    store_row<DB>(out + (pl.img + pixel(pl.win, n)) * g.C + pl.hd * g.d, O, g.d, hf, inv);
+}
+
+// dq and the bias's gradient; the second kernel's -LSE * log2 e and -delta of every row.
+template <int DB, bool CKPT, bool ALN, int W, bool HIST>
+__global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias bi, int nblk, int prows, const float *__restrict__ q,
+                                                       const float *__restrict__ k, const float *__restrict__ v,
+                                                       const uint8_t *__restrict__ ckpt, const float *__restrict__ out,
+                                                       const float *__restrict__ dout, const float *__restrict__ lse,
+                                                       float *__restrict__ dq, float2 *__restrict__ ext, float *__restrict__ part)
+{
+    constexpr int NT = 64 * W, SB = 32 * W;
+    using I = Img<DB>;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    float *S = (float *)smem;
+    int *map = (int *)(smem + stage_bytes<DB>());
+    float *B = (float *)(map + 2 * g.M);
+    double *H = (double *)(B + ((bi.rows * bi.w2 + 1) & ~1));
+    const int hsize = bi.hrows * bi.w2;
+    const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place pl = place_of(g, nblk, NT, map);
+    if (HIST)
+        for (int e = threadIdx.x; e < W * hsize; e += NT) H[e] = 0.;
+    __syncthreads();
+    const int first = pl.blk * SB, last = first + SB < g.N ? first + SB - 1 : g.N - 1, n0 = first + wave * 32, n = n0 + col;
+    const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m), nc = n < g.N ? n : g.N - 1;
+    const bool active = n0 < g.N;
+    Raw Q[4 * DB], D[4 * DB];
+    operand<DB, false>(g, pl, rows_of_grid(g, pl, dout, g.C), nc, 1.f, D);
+    float delta = 0.f;
+    {
+        Raw O[4 * DB];
+        operand<DB, false>(g, pl, rows_of_grid(g, pl, out, g.C), nc, 1.f, O);
+#pragma unroll
+        for (int i = 0; i < 4 * DB; ++i) delta += (O[i].x * D[i].x + O[i].y * D[i].y) + (O[i].z * D[i].z + O[i].w * D[i].w);
+        delta += __shfl_xor(delta, 32);
+    }
+    operand<DB, CKPT>(g, pl, CKPT ? rows_of_ckpt(g, pl, ckpt, 0) : rows_of_grid(g, pl, q, g.tstride), nc, g.scale_c * kLog2e, Q);
+    const float e0 = lse[(int64_t)pl.u * g.N + nc], L = n >= g.N || e0 == -INFINITY ? bf::kNoRow : e0 * kLog2e;
+    if (n < g.N && hf == 0) ext[(int64_t)pl.u * g.N + n] = float2{-L, -delta};
+    const int mylin = lin(g, nc), wsy1 = row_of(n0 + 31 < g.N ? n0 + 31 : g.N - 1, g.inv_m);
+    const Rows ks = CKPT ? rows_of_ckpt(g, pl, ckpt, 1) : rows_of_grid(g, pl, k, g.tstride);
+    const Rows vs = CKPT ? rows_of_ckpt(g, pl, ckpt, 2) : rows_of_grid(g, pl, v, g.tstride);
+    f32x16 A[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) A[db][i] = 0.f;
+    const int ntiles = (g.N + kTile - 1) / kTile;
+    const f32x16 z = {0};
+    Mover<DB, W, CKPT, CKPT, false> mv;
+    mv.request(g, pl.win, ks, vs, nullptr, 0);
+    mv.commit(g, S, 0, 1.f);
+    mv.request(g, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
+    int before = -1;
+    for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
+        const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
+        const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
+        stage_bias<-1>(g, bi, ch, pl.hd, kLog2e, B, NT);
+        double *const mine = H + wave * hsize + ch.c0 - (sy1 - wsy1) * bi.w2 - mylin;
+        __syncthreads();
+        for (int tile = t0; tile < t1; ++tile) {
+            const float *cur = S + (tile & 1) * I::STAGE;
+            if (tile + 1 < ntiles) {
+                mv.commit(g, S + ((tile + 1) & 1) * I::STAGE, tile + 1, 1.f);
+                mv.request(g, pl.win, ks, vs, nullptr, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
+            }
+            if (active) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const int key0 = tile * kTile + kb * 32;
+                    if (!ALN && key0 >= g.N) break;
+                    const Words16<ALN> wd = words_of<ALN>(g, (const int *)(cur + I::LT), tile, kb, hf);
+                    const float *row = cur + (kb * 32 + col) * I::STR + 4 * hf;
+                    f32x16 s = scores<DB>(row, Q, bias_block<ALN>(B + ch.c0 - mylin, wd), g.d);
+                    const f32x16 p = scores<DB>(row + I::YR, D, z, g.d);
+                    if (!ALN) mask_rows(s, key0, g.N, hf);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] - L) * (p[i] - delta);
+                    if (HIST) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            __hip_atomic_fetch_add(mine + wd(i), (double)s[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                    }
+                    contract<DB>(A, cur + (kb * 32 + 4 * hf) * I::STR + col, s);
+                }
+            }
+            __syncthreads();
+        }
+        if (HIST) {
+            flush<W, 32>(g, bi, ch, H, hsize, first, sy0, sy1, before,
+                         part + ((int64_t)pl.u * nblk + pl.blk) * prows * bi.w2 + ch.ty0 * bi.w2);
+            before = ch.ty1;
+        }
+    }
+    if (n >= g.N) return;
+    store_row<DB>(dq + (pl.img + pixel(pl.win, n)) * g.C + pl.hd * g.d, A, g.d, hf, g.scale_c);
+}
+
+template <int DB, bool CKPT, bool ALN, int W>
+__global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias bi, int nblk, const float *__restrict__ q, const float *__restrict__ k,
+                                                        const float *__restrict__ v, const uint8_t *__restrict__ ckpt,
+                                                        const float *__restrict__ dout, const float2 *__restrict__ ext,
+                                                        float *__restrict__ dk, float *__restrict__ dv)
+{
+    constexpr int NT = 64 * W, SB = 32 * W;
+    using I = Img<DB>;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    float *S = (float *)smem;
+    int *map = (int *)(smem + stage_bytes<DB>());
+    float *B = (float *)(map + 2 * g.M);
+    const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place pl = place_of(g, nblk, NT, map);
+    __syncthreads();
+    const int first = pl.blk * SB, last = first + SB < g.N ? first + SB - 1 : g.N - 1, n0 = first + wave * 32, n = n0 + col;
+    const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m), nc = n < g.N ? n : g.N - 1;
+    const bool active = n0 < g.N;
+    Raw Kb[4 * DB], Vb[4 * DB];
+    operand<DB, CKPT>(g, pl, CKPT ? rows_of_ckpt(g, pl, ckpt, 1) : rows_of_grid(g, pl, k, g.tstride), nc, 1.f, Kb);
+    operand<DB, CKPT>(g, pl, CKPT ? rows_of_ckpt(g, pl, ckpt, 2) : rows_of_grid(g, pl, v, g.tstride), nc, 1.f, Vb);
+    const int mylin = lin(g, nc);
+    const Rows qs = CKPT ? rows_of_ckpt(g, pl, ckpt, 0) : rows_of_grid(g, pl, q, g.tstride), ds = rows_of_grid(g, pl, dout, g.C);
+    const float2 *const ex = ext + (int64_t)pl.u * g.N;
+    f32x16 Ak[DB], Av[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) Ak[db][i] = 0.f, Av[db][i] = 0.f;
+    const int ntiles = (g.N + kTile - 1) / kTile;
+    const float scale = g.scale_c * kLog2e;
+    Mover<DB, W, CKPT, false, true> mv;
+    mv.request(g, pl.win, qs, ds, ex, 0);
+    mv.commit(g, S, 0, scale);
+    mv.request(g, pl.win, qs, ds, ex, ntiles > 1 ? 1 : 0);
+    for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
+        const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
+        const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
+        stage_bias<1>(g, bi, ch, pl.hd, kLog2e, B, NT);
+        __syncthreads();
+        for (int tile = t0; tile < t1; ++tile) {
+            const float *cur = S + (tile & 1) * I::STAGE;
+            if (tile + 1 < ntiles) {
+                mv.commit(g, S + ((tile + 1) & 1) * I::STAGE, tile + 1, scale);
+                mv.request(g, pl.win, qs, ds, ex, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
+            }
+            if (active) {
+#pragma unroll
+                for (int qb = 0; qb < 2; ++qb) {
+                    if (!ALN && tile * kTile + qb * 32 >= g.N) break;
+                    const Words16<ALN> wd = words_of<ALN>(g, (const int *)(cur + I::LT), tile, qb, hf);
+                    const float *row = cur + (qb * 32 + col) * I::STR + 4 * hf;
+                    f32x16 s = bias_block<ALN>(B + ch.c0 - mylin, wd), p;
+#pragma unroll
+                    for (int a = 0; a < 4; ++a) {
+                        const float4 l = *(const float4 *)(cur + I::EX + qb * 32 + 8 * a + 4 * hf), dl = *(const float4 *)(cur + I::EX + kTile + qb * 32 + 8 * a + 4 * hf);
+                        s[4 * a] += l.x, s[4 * a + 1] += l.y, s[4 * a + 2] += l.z, s[4 * a + 3] += l.w;
+                        p[4 * a] = dl.x, p[4 * a + 1] = dl.y, p[4 * a + 2] = dl.z, p[4 * a + 3] = dl.w;
+                    }
+                    s = scores<DB>(row, Kb, s, g.d);
+                    p = scores<DB>(row + I::YR, Vb, p, g.d);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        s[i] = __builtin_amdgcn_exp2f(s[i]);
+                        p[i] *= s[i];
+                    }
+                    contract<DB>(Av, cur + I::YR + (qb * 32 + 4 * hf) * I::STR + col, s);
+                    contract<DB>(Ak, cur + (qb * 32 + 4 * hf) * I::STR + col, p);
+                }
+            }
+            __syncthreads();
+        }
+    }
+    if (n >= g.N) return;
+    const int64_t at = (pl.img + pixel(pl.win, n)) * g.C + pl.hd * g.d;
+    store_row<DB>(dk + at, Ak, g.d, hf, kLn2);          // (Q carries scale * log2 e)
+    store_row<DB>(dv + at, Av, g.d, hf, 1.f);
+}
+
+constexpr size_t kBiasBytes = 36 * 1024, kHistBytes = 9 * 1024;
+
+template <int DB, bool ALN, int W>
+hipError_t launch_fwd_one(const Geo &g, const FwdArgs &a)
+{
+    Bias bi{a.bias, 0, 0, 0, 0};
+    plan_chunks(g, RIB_F32, &bi, false, kBiasBytes, 0);
+    const int nblk = (g.N + 32 * W - 1) / (32 * W);
+    const size_t smem = stage_bytes<DB>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.w2 * 4;
+    if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
+    auto kern = fwd_kernel<DB, ALN, W>;
+    const hipError_t e = prepare_kernel((const void *)kern, nullptr);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * nblk)), dim3(64 * W), smem, a.st, g, bi, nblk, a.force_max, (const float *)a.q,
+                       (const float *)a.k, (const float *)a.v, (float *)a.out, a.lse);
+    return hipGetLastError();
+}
+template <int DB>
+hipError_t launch_fwd_width(const Geo &g, const FwdArgs &a)
+{
+    if (g.N <= 32) return launch_fwd_one<DB, false, 1>(g, a);
+    return g.M % 8 == 0 ? launch_fwd_one<DB, true, 4>(g, a) : launch_fwd_one<DB, false, 4>(g, a);
+}
+
+template <int DB, bool CKPT, bool ALN, int W, bool HIST>
+hipError_t launch_dq_one(const Geo &g, const BwdArgs &a, const Ws &ws)
+{
+    Bias bi{a.bias, 0, 0, 0, 0};
+    plan_chunks(g, RIB_F32, &bi, HIST, kBiasBytes, kHistBytes);
+    const size_t smem = stage_bytes<DB>() + 8 * (size_t)g.M + ((size_t)bi.rows * bi.w2 + 1) / 2 * 8 + (size_t)W * bi.hrows * bi.w2 * 8;
+    if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
+    auto kern = dq_kernel<DB, CKPT, ALN, W, HIST>;
+    const hipError_t e = prepare_kernel((const void *)kern, nullptr);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * ws.nblk)), dim3(64 * W), smem, a.st, g, bi, ws.nblk, ws.prows, (const float *)a.q,
+                       (const float *)a.k, (const float *)a.v, a.ckpt, (const float *)a.out, (const float *)a.dout, a.lse, (float *)a.dq,
+                       (float2 *)((char *)a.ws + ws.ext), (float *)((char *)a.ws + ws.part));
+    return hipGetLastError();
+}
+template <int DB, bool CKPT, bool ALN, int W>
+hipError_t launch_pair(const Geo &g, const BwdArgs &a, const Ws &ws)
+{
+    hipError_t e = a.dbias != nullptr ? launch_dq_one<DB, CKPT, ALN, W, true>(g, a, ws) : launch_dq_one<DB, CKPT, ALN, W, false>(g, a, ws);
+    if (e != hipSuccess) return e;
+    Bias bi{a.bias, 0, 0, 0, 0};
+    plan_chunks(g, RIB_F32, &bi, false, kBiasBytes, 0);
+    const size_t smem = stage_bytes<DB>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.w2 * 4;
+    if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
+    auto kern = dkv_kernel<DB, CKPT, ALN, W>;
+    e = prepare_kernel((const void *)kern, nullptr);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * ws.nblk)), dim3(64 * W), smem, a.st, g, bi, ws.nblk, (const float *)a.q,
+                       (const float *)a.k, (const float *)a.v, a.ckpt, (const float *)a.dout, (const float2 *)((const char *)a.ws + ws.ext),
+                       (float *)a.dk, (float *)a.dv);
+    return hipGetLastError();
+}
+template <int DB, bool CKPT>
+hipError_t launch_bwd_src(const Geo &g, const BwdArgs &a, const Ws &ws)
+{
+    if (g.N <= 32) return launch_pair<DB, CKPT, false, 1>(g, a, ws);
+    return g.M % 8 == 0 ? launch_pair<DB, CKPT, true, 4>(g, a, ws) : launch_pair<DB, CKPT, false, 4>(g, a, ws);
+}
+template <int DB>
+hipError_t launch_bwd_width(const Geo &g, const BwdArgs &a, const Ws &ws)
+{
+    return a.ckpt != nullptr ? launch_bwd_src<DB, true>(g, a, ws) : launch_bwd_src<DB, false>(g, a, ws);
+}
+
+}  // namespace fp
+
+hipError_t launch_fwd_f32(const Geo &g, const FwdArgs &a)
+{
+    return g.d <= 32 ? fp::launch_fwd_width<1>(g, a) : fp::launch_fwd_width<2>(g, a);
+}
+
+hipError_t launch_bwd_f32(const Geo &g, const BwdArgs &a)
+{
+    const Ws ws = ws_layout(g, RIB_F32);
+    const hipError_t e = g.d <= 32 ? fp::launch_bwd_width<1>(g, a, ws) : fp::launch_bwd_width<2>(g, a, ws);
+    if (e != hipSuccess || a.dbias == nullptr) return e;
+    return launch_reduce(g, RIB_F32, ws, (const float *)((const char *)a.ws + ws.part), a.dbias, a.st);
+}
+
+}  // namespace rpb
+}  // namespace rib

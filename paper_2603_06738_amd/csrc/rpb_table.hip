@@ -1,0 +1,128 @@
+// The learned relative position bias itself: offsets from buckets, the sum of the attention backward's partial gradients, and
+// the buckets' gradient.  Operators: include/rib_attn.h.
+#include "rpb_common.h"
+
+namespace rib {
+namespace rpb {
+namespace {
+
+// bias[head][o] = table[head][index[o]].  Bound by memory, and by its launch at most sizes.
+template <class T>
+__global__ __launch_bounds__(256) void table_fwd_kernel(int L, int buckets, const T *__restrict__ table, const int32_t *__restrict__ index,
+                                                        float *__restrict__ bias)
+{
+    const int o = blockIdx.x * 256 + threadIdx.x, hd = blockIdx.y;
+    if (o >= L) return;
+    const int i = index[o];
+    float x = -INFINITY;
+    if ((uint32_t)i < (uint32_t)buckets) {
+        x = widen(table[(int64_t)hd * buckets + i]);
+        if (x <= kExcluded) x = -INFINITY;
+    }
+    bias[(int64_t)hd * L + o] = x;
+}
+
+// dtable[head][b] = sum of dbias[head][o] over the offsets of bucket b.
+//
+// Many offsets share a bucket, so their values are added in LDS, as 64-bit whole numbers: such sums do not depend on the order of
+// the additions.  The unit is the largest value of the head over 2^(62 - bits of the number of offsets), so sums cannot overflow and a
+// bucket whose gradient is 2^-21 of the largest still has 24 bits.  Values that are not finite are noted by kind beside the sums.
+constexpr int kBuckets = 2048;          // buckets a workgroup
+template <class T>
+__global__ __launch_bounds__(1024) void table_bwd_kernel(int L, int buckets, int bits, const float *__restrict__ dbias,
+                                                         const int32_t *__restrict__ index, T *__restrict__ dtable)
+{
+    __shared__ unsigned long long sum[kBuckets];
+    __shared__ uint32_t odd[kBuckets];
+    __shared__ uint32_t top;
+    const int hd = blockIdx.y, b0 = blockIdx.x * kBuckets, tid = threadIdx.x;
+    const float *x = dbias + (int64_t)hd * L;
+    if (tid == 0) top = 0u;
+    for (int i = tid; i < kBuckets; i += 1024) sum[i] = 0ull, odd[i] = 0u;
+    __syncthreads();
+    uint32_t m = 0u;
+    for (int o = tid; o < L; o += 1024) {
+        const uint32_t a = __float_as_uint(x[o]) & 0x7fffffffu;
+        if (a < 0x7f800000u && a > m) m = a;
+    }
+    atomicMax(&top, m);
+    __syncthreads();
+    int e;
+    frexp((double)__uint_as_float(top), &e);            // the largest is below 2^e
+    const double unit = ldexp(1., e + bits - 62);
+    const double per = ldexp(1., 62 - bits - e);
+    for (int o = tid; o < L; o += 1024) {
+        const int i = index[o] - b0;
+        if ((uint32_t)index[o] >= (uint32_t)buckets || (uint32_t)i >= (uint32_t)kBuckets) continue;
+        const float v = x[o];
+        if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) atomicOr(&odd[i], v != v ? 4u : v > 0.f ? 1u : 2u);
+        else atomicAdd(&sum[i], (unsigned long long)llrint((double)v * per));
+    }
+    __syncthreads();
+    for (int i = tid; i < kBuckets && b0 + i < buckets; i += 1024) {
+        float v = (float)((double)(long long)sum[i] * unit);
+        if (odd[i] != 0u) v = odd[i] == 1u ? INFINITY : odd[i] == 2u ? -INFINITY : NAN;
+        store_as(dtable + (int64_t)hd * buckets + b0 + i, v);
+    }
+}
+
+// dbias[head][o] = sum over windows and their workgroups of the workgroups' sums.  64 offsets a workgroup, 16 runs of windows, each
+// in ascending order, then the runs in ascending order.  Bound by memory: every partial sum is read once.
+__global__ __launch_bounds__(1024) void reduce_kernel(Geo g, int windows, int nblk, int prows, int group, const float *__restrict__ part,
+                                                      float *__restrict__ dbias)
+{
+    __shared__ float run[16][64];
+    const int w2 = 2 * g.M - 1, L = w2 * w2, hd = blockIdx.y;
+    const int lane = threadIdx.x & 63, r = threadIdx.x >> 6, o = blockIdx.x * 64 + lane;
+    const int per = (windows + 15) / 16, w0 = r * per, w1 = w0 + per < windows ? w0 + per : windows;
+    float sum = 0.f;
+    if (o < L)
+        for (int blk = 0; blk < nblk; ++blk) {
+            const int first = blk * group, last = first + group < g.N ? first + group - 1 : g.N - 1;
+            const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m);
+            // the offset's word of this workgroup's rows (streamed - stationary row, from -sy1 on, is minus the offset's)
+            const int at = 2 * g.M * (g.M - 1) + sy1 * w2 + g.M - 1 - o;
+            if (at < 0 || at >= (g.M + sy1 - sy0) * w2) continue;
+            const float *p = part + ((int64_t)w0 * g.heads + hd) * nblk * prows * w2 + (int64_t)blk * prows * w2 + at;
+            const int64_t step = (int64_t)g.heads * nblk * prows * w2;
+#pragma unroll 4
+            for (int w = w0; w < w1; ++w, p += step) sum += *p;
+        }
+    run[r][lane] = sum;
+    __syncthreads();
+    if (r == 0 && o < L) {
+        for (int i = 1; i < 16; ++i) sum += run[i][lane];
+        dbias[(int64_t)hd * L + o] = sum;
+    }
+}
+
+}  // namespace
+
+hipError_t launch_reduce(const Geo &g, int dtype, const Ws &w, const float *part, float *dbias, hipStream_t st)
+{
+    const int L = (2 * g.M - 1) * (2 * g.M - 1);
+    hipLaunchKernelGGL(reduce_kernel, dim3((L + 63) / 64, g.heads), dim3(1024), 0, st, g, (int)(g.units / g.heads), w.nblk, w.prows,
+                       group_tokens(dtype, g.N), part, dbias);
+    return hipGetLastError();
+}
+hipError_t launch_table_fwd(int M, int heads, int buckets, int dtype, const void *table, const int32_t *index, float *bias, hipStream_t st)
+{
+    const int L = (2 * M - 1) * (2 * M - 1);
+    const dim3 grid((L + 255) / 256, heads);
+    if (dtype == RIB_BF16) hipLaunchKernelGGL(table_fwd_kernel<bf16_t>, grid, dim3(256), 0, st, L, buckets, (const bf16_t *)table, index, bias);
+    else hipLaunchKernelGGL(table_fwd_kernel<float>, grid, dim3(256), 0, st, L, buckets, (const float *)table, index, bias);
+    return hipGetLastError();
+}
+hipError_t launch_table_bwd(int M, int heads, int buckets, int dtype, const float *dbias, const int32_t *index, void *dtable, hipStream_t st)
+{
+    const int L = (2 * M - 1) * (2 * M - 1);
+    int bits = 1;
+    while ((1 << bits) < L) ++bits;
+    const dim3 grid((buckets + kBuckets - 1) / kBuckets, heads);
+    if (dtype == RIB_BF16) hipLaunchKernelGGL(table_bwd_kernel<bf16_t>, grid, dim3(1024), 0, st, L, buckets, bits, dbias, index, (bf16_t *)dtable);
+    else hipLaunchKernelGGL(table_bwd_kernel<float>, grid, dim3(1024), 0, st, L, buckets, bits, dbias, index, (float *)dtable);
+    return hipGetLastError();
+}
+
+}  // namespace rpb
+}  // namespace rib

@@ -1,0 +1,124 @@
+"""Window attention with a learned relative position bias on the GPU, every element of every result against the plain
+64-bit form, within bounds that follow from the kernels' roundings (tests/rpb_reference.py)."""
+import itertools
+
+import numpy as np
+import pytest
+import torch
+
+import rpb_reference as ref
+from paper_2603_06738_amd import binding as rb
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def storage(x, dtype):
+    t = torch.from_numpy(np.ascontiguousarray(x)).float()
+    return t.to(torch.bfloat16) if dtype == "bf16" else t
+
+
+class Case:
+    """Tensors of one call on the GPU, and their values in 64 bits."""
+
+    def __init__(self, dtype, B, H, W, heads, d, M, s, buckets="full", packed=False, scale=None, seed=0, spread=1.0, table_std=0.5,
+                 flags=0):
+        rng = np.random.default_rng(seed)
+        self.dtype, self.B, self.H, self.W, self.heads, self.d, self.M, self.s = dtype, B, H, W, heads, d, M, s
+        self.scale = d ** -0.5 if scale is None else scale
+        self.C, self.N = heads * d, M * M
+        self.u = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+        self.td = torch.bfloat16 if dtype == "bf16" else torch.float32
+        qkv = storage(rng.standard_normal((B, H, W, 3 * self.C)) * spread, dtype)
+        self.qkv = qkv.to(DEV)
+        parts = [self.qkv[..., i * self.C:(i + 1) * self.C] for i in range(3)]
+        self.q, self.k, self.v = parts if packed else [x.contiguous() for x in parts]
+        self.dout = storage(rng.standard_normal((B, H, W, self.C)), dtype).to(DEV)
+        self.index_np, self.nb = ref.bucket_index(buckets, M)
+        self.table = storage(rng.standard_normal((heads, self.nb)) * table_std, dtype).to(DEV)
+        self.index = torch.from_numpy(self.index_np).to(DEV)
+        self.p = rb.make_params(B, H, W, heads, d, 0, M, s, self.scale, 0.0, dtype, flags=flags, token_stride=3 * self.C if packed else 0)
+        self.tp = rb.make_rpb_params(M, heads, self.nb, dtype)
+        L, nw = (2 * M - 1) ** 2, B * (H // M) * (W // M)
+        f32 = torch.float32
+        self.bias, self.dbias = self.nan(heads, L, dtype=f32), self.nan(heads, L, dtype=f32)
+        self.lse = self.nan(nw, heads, self.N, dtype=f32)
+        self.out, self.dq, self.dk, self.dv = (self.nan(B, H, W, self.C) for _ in range(4))
+        self.dtable = self.nan(heads, self.nb)
+        self.ws = torch.full((max(rb.rib_rpb_attn_bwd_workspace_bytes(self.p), 256),), 0xff, dtype=torch.uint8, device=DEV)
+
+    def nan(self, *shape, dtype=None):
+        return torch.full(shape, float("nan"), dtype=dtype or self.td, device=DEV)
+
+    def forward(self):
+        rb.rib_rpb_table_fwd(self.tp, self.table, self.index, self.bias)
+        rb.rib_rpb_attn_fwd(self.p, self.q, self.k, self.v, self.bias, self.out, self.lse)
+
+    def backward(self):
+        rb.rib_rpb_attn_bwd(self.p, self.q, self.k, self.v, self.bias, self.out, self.dout, self.lse, self.dq, self.dk, self.dv,
+                            self.dbias, self.ws)
+        rb.rib_rpb_table_bwd(self.tp, self.dbias, self.index, self.dtable)
+
+    def reference(self, backward=True, bwd_qkv=None):
+        g = [np64(x) for x in (self.q, self.k, self.v)]
+        bias = ref.bias_of(np64(self.table), self.index_np)
+        kw = dict(out=np64(self.out), dout=np64(self.dout), bwd_qkv=bwd_qkv) if backward else {}
+        return ref.attention(*g, bias, self.heads, self.M, self.s, self.scale, self.u, **kw)
+
+
+def np64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def close(name, got, want, tol):
+    got = np64(got)
+    inf = np.isinf(want)
+    assert np.array_equal(got[inf], want[inf]), name
+    off = np.abs(np.where(inf, 0, got - np.where(inf, 0, want)))
+    assert not np.isnan(off).any(), f"{name}: NaN"
+    worst = np.unravel_index(np.argmax(off - tol), off.shape)
+    assert (off <= tol).all(), f"{name} at {worst}: {got[worst]} for {want[worst]}, {off[worst]:.3g} off, {tol[worst]:.3g} allowed"
+
+
+def check(c, R, backward=True):
+    close("lse", c.lse, R.lse, R.lse_tol)
+    close("out", c.out, R.out, R.out_tol)
+    if not backward:
+        return
+    for n in ("dq", "dk", "dv", "dbias"):
+        close(n, getattr(c, n), getattr(R, n), getattr(R, n + "_tol"))
+    want = ref.table_grad(R.dbias, c.index_np, c.nb)
+    close("dtable", c.dtable, want, ref.table_grad(R.dbias_tol, c.index_np, c.nb) + c.u * np.abs(want) + 1e-30)
+
+
+def run(*a, **kw):
+    c = Case(*a, **kw)
+    c.forward()
+    c.backward()
+    check(c, c.reference())
+    return c
+
+
+# window sides over every tile edge: a single token, partial tiles, one wave, whole tiles, several workgroups
+SIDES = [1, 2, 3, 5, 6, 7, 8, 9, 11, 12, 16, 17, 20, 24]
+
+
+@pytest.mark.parametrize("dtype,M", itertools.product(("bf16", "f32"), SIDES))
+def test_window_sides(dtype, M):
+    nwy, nwx = (3, 2) if M <= 12 else (1, 2)
+    run(dtype, 1, nwy * M, nwx * M, 2, 30, M, M // 2, seed=M)
+
+
+@pytest.mark.parametrize("dtype,d", itertools.product(("bf16", "f32"), (1, 2, 3, 7, 8, 10, 15, 16, 31, 32, 33, 34, 46, 47, 48, 62, 63, 64)))
+def test_head_dims(dtype, d):
+    run(dtype, 1, 16, 24, 1 if d % 2 else 2, d, 8, 3, seed=d)
+    run(dtype, 1, 18, 9, 1, d, 9, 0, seed=d, packed=True)
+
+
+@pytest.mark.parametrize("dtype,M,kind", itertools.product(("bf16", "f32"), (4, 7, 16, 18), ("coarse", "near", "past", "none", "one")))
+def test_bucket_maps(dtype, M, kind):
+    c = run(dtype, 2, M, 2 * M, 3, 30, M, 1, buckets=kind, packed=True, seed=3)
+    if kind == "past":
+        assert torch.isinf(c.lse[:, :, 0]).all()
+    if kind == "none":
+        assert (c.out == 0).all() and (c.dq == 0).all() and (c.dk == 0).all() and (c.dv == 0).all() and (c.dbias == 0).all()
