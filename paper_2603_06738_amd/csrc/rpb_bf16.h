@@ -5,11 +5,11 @@
 // tiles of 64 token rows, two stages in turn.  Scores are 32x32 blocks with the streamed tokens as rows, so a lane owns one
 // stationary token and 16 streamed ones; their bias is the C operand of the score product.  What is packed to bf16 there
 // (P, dS) is the B operand of the product that contracts over the streamed tokens, whose A operand is read transposed from
-// the same rows.  Q carries scale * log2 e, rounded to bf16 once, in all three kernels, so that the backward makes the
-// forward's logits again bit for bit.
+// the same rows.  Products of q and k are exact in fp32 and scaled there: rounding a scaled q to bf16 would save 16 of some 100 vector
+// instructions a block, and cost as much accuracy as the rounding of P.
 //
-// The backward's -LSE and -delta ride in two more columns of Q's and dO's rows, as bf16 pairs (high and low part), against
-// ones in K's and V's: the products are then S - LSE and dP - delta.
+// The backward's -delta rides in two more columns of dO's rows, as a bf16 pair (high and low part, 2^-16 of it is lost), against
+// ones in V's: the product is then dP - delta.  Where the query is streamed (dkv), -LSE does the same beside q and k.
 #pragma once
 
 #include "rpb_common.h"
@@ -21,7 +21,7 @@ namespace bf {
 using namespace rows;
 
 constexpr uint32_t kOnes = 0x3f803f80u;
-constexpr float kNoRow = 1e30f;         // in place of LSE * log2 e where a row has no key: every probability is zero
+constexpr float kNoRow = 1e30f;         // in place of LSE where a row has no key: every probability is zero
 
 // LDS image of a tile: X and Y rows, a streamed token's lin().  K: columns of the contracted width.
 template <int KX, int KY>
@@ -140,7 +140,7 @@ struct Mover {
             const bool in = ALN || n < g.N;
             bf16_t *xr = S + row * I::XS, *yr = S + I::YR + row * I::YS;
             Raw a = widen_piece<SX>(x[p]), b = widen_piece<SY>(y[p]);
-            if (EXT) a = scaled(a, scale);
+            if (EXT && scale != 1.f) a = scaled(a, scale);
             if (!in) b.w[0] = b.w[1] = b.w[2] = b.w[3] = 0u;    // (an infinity in the repeated last token must not meet P = 0)
             if (ONES && SX == kCkpt && piece_col<SX>(j, g.d) == KX - 8) a.w[3] = kOnes;
             if (ONES && SY == kCkpt && piece_col<SY>(j, g.d) == KY - 8) b.w[3] = kOnes;
@@ -196,21 +196,16 @@ __device__ __forceinline__ void stationary_rows(const Geo &g, const Win &win, co
     for (int b = 0; b < 2; ++b) read_rows<K / 16>(B[b], area + (b * 32 + (lane & 31)) * STR + 8 * (lane >> 5));
     __builtin_amdgcn_wave_barrier();
 }
-struct FixNone {
-    __device__ __forceinline__ Raw operator()(int, const Raw &r) const { return r; }
-    __device__ __forceinline__ void columns(bf16_t *, int) const {}
-};
 struct FixScale {
-    float s;
-    __device__ __forceinline__ Raw operator()(int, const Raw &r) const { return scaled(r, s); }
+    float s;            // (1: values as they are)
+    __device__ __forceinline__ Raw operator()(int, const Raw &r) const { return s != 1.f ? scaled(r, s) : r; }
     __device__ __forceinline__ void columns(bf16_t *, int) const {}
 };
 // The pair `w` of row `lane` in the last two columns.
 template <int K>
 struct FixPair {
-    float s;            // 0: values as they are
     uint32_t w;
-    __device__ __forceinline__ Raw operator()(int, const Raw &r) const { return s != 0.f ? scaled(r, s) : r; }
+    __device__ __forceinline__ Raw operator()(int, const Raw &r) const { return r; }
     __device__ __forceinline__ void columns(bf16_t *area, int str) const { *(uint32_t *)(area + (threadIdx.x & 63) * str + K - 2) = w; }
 };
 
@@ -245,6 +240,15 @@ __device__ __forceinline__ f32x16 bias_block(const float *mine, const Words16<AL
 #pragma unroll
     for (int i = 0; i < 16; ++i) c[i] = mine[w(i)];
     return c;
+}
+
+// Adds a block of dS to the wave's sums by offset, in 64 bits (LDS adds doubles 20 times as fast as floats: 55 and 1290 ns for a wave's 16).
+// The sums are the wave's own and its additions happen in its order, so they do not depend on what other waves do.
+template <bool ALN>
+__device__ __forceinline__ void add_offsets(double *mine, const Words16<ALN> &w, const f32x16 &v)
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i) __hip_atomic_fetch_add(mine + w(i), (double)v[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
 }
 
 // Channels 8 (i / 4) + 4 hf .. + 3 of block `db` of a token's row, times `s`.
@@ -306,7 +310,7 @@ constexpr size_t stage_bytes()
 // ---- forward -----------------------------------------------------------------------------------------------------
 
 // One walk over the keys.  MAX: with the running maximum of every row.
-template <bool MAX, int KX, int DB, bool SUM, int SRC, bool ALN, int W>
+template <bool MAX, int KX, int DB, bool SUM, int SRC, bool ALN, bool CARRY, int W>
 __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Place &pl, const Rows &ks, const Rows &vs, bf16_t *S, float *B,
                                          const bf16x8 (&Q)[2][KX / 16], f32x16 (&O)[2][DB], float (&sum)[2], float (&top)[2], int sy0, int sy1,
                                          const int (&mylin)[2], bool active)
@@ -328,11 +332,13 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
     mv.request(g, pl.win, ks, vs, nullptr, 0);
     mv.template commit<KX, KY, false, ALN>(g, S, 0, 1.f);
     mv.request(g, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
+    f32x16 next;            // (CARRY) the bias of block (1, the coming one)
     for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
         const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
         const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
-        stage_bias<-1>(g, bi, ch, pl.hd, kLog2e, B, NT);
+        stage_bias<-1>(g, bi, ch, pl.hd, bi.bs, B, NT);
         __syncthreads();
+        if (CARRY && t0 == 0 && active) next = bias_block<ALN>(B + ch.c0 - mylin[1], words_of<ALN>(g, nullptr, 0, 0, hf));
         for (int tile = t0; tile < t1; ++tile) {
             const bf16_t *cur = S + (tile & 1) * I::STAGE;
             if (tile + 1 < ntiles) {
@@ -352,11 +358,15 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
 #pragma unroll
                         for (int i = 0; i < 2; ++i) At[db][i] = read_tr<I::YS>(cur + I::YR + (kb * 32 + 16 * i) * I::YS, tro, 32 * db);
 #pragma unroll
-                    for (int qb = 0; qb < 2; ++qb) {
-                        f32x16 s = bias_block<ALN>(B + ch.c0 - mylin[qb], wd);
+                    for (int qx = 0; qx < 2; ++qx) {
+                        const int qb = 1 - qx;
+                        f32x16 s = CARRY && qb == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[qb], wd);
+                        if (CARRY && qb == 0) next = s;
 #pragma unroll
                         for (int i = 0; i < KX / 16; ++i) s = mfma(Ak[i], Q[qb][i], s);
                         if (!ALN) mask_rows(s, key0, g.N, hf);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] *= bi.c;
                         if (MAX) {
                             float m = s[0];
 #pragma unroll
@@ -403,7 +413,7 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
     }
 }
 
-template <int KX, int DB, bool SUM, int SRC, bool ALN, int W>
+template <int KX, int DB, bool SUM, int SRC, bool ALN, bool CARRY, int W>
 __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void fwd_kernel(Geo g, Bias bi, int nblk, int force_max, const bf16_t *__restrict__ q,
                                                         const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
                                                         bf16_t *__restrict__ out, float *__restrict__ lse)
@@ -420,7 +430,7 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void fwd_kernel(Geo g, Bias
     const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m);
     const bool active = n0 < g.N;
     bf16x8 Q[2][KX / 16];
-    stationary_rows<KX, LP, SRC>(g, pl.win, grid_rows(g, pl, q, g.tstride), n0, S + wave * 64 * (KX + 8), Q, FixScale{g.scale_c * kLog2e});
+    stationary_rows<KX, LP, SRC>(g, pl.win, grid_rows(g, pl, q, g.tstride), n0, S + wave * 64 * (KX + 8), Q, FixScale{bi.qs});
     int mylin[2];
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
@@ -434,16 +444,16 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void fwd_kernel(Geo g, Bias
     f32x16 O[2][DB];
     float sum[2], top[2];
     // First without a running maximum: exp2 of a logit is a normal number far beyond what bounded logits need.  A row whose
-    // denominator leaves [2^-60, 2^60] sends the workgroup on a second walk, with one.
+    // denominator leaves [2^-60, 2^60], and not for want of keys, sends the workgroup on a second walk, with one.
     bool bad = true;
     if (!force_max) {
-        fwd_walk<false, KX, DB, SUM, SRC, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, sy0, sy1, mylin, active);
+        fwd_walk<false, KX, DB, SUM, SRC, ALN, CARRY, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, sy0, sy1, mylin, active);
         bad = false;
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb)
-            if (active && !((sum[qb] >= 0x1p-60f) && (sum[qb] <= 0x1p60f))) bad = true;
+            if (active && bad_rows(g, bi, pl.hd, n0 + qb * 32 + col, sum[qb])) bad = true;
     }
-    if (__syncthreads_or(bad)) fwd_walk<true, KX, DB, SUM, SRC, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, sy0, sy1, mylin, active);
+    if (__syncthreads_or(bad)) fwd_walk<true, KX, DB, SUM, SRC, ALN, CARRY, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, sy0, sy1, mylin, active);
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
         const int n = n0 + qb * 32 + col;
@@ -459,7 +469,7 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void fwd_kernel(Geo g, Bias
 
 // ---- backward: dq and the bias's gradient -------------------------------------------------------------------------
 
-template <int K, int DB, int SRC, int SG, bool ALN, int W, bool HIST>
+template <int K, int DB, int SRC, int SG, bool ALN, bool CARRY, int W, bool HIST>
 __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias bi, int nblk, int prows, const bf16_t *__restrict__ q,
                                                        const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
                                                        const uint8_t *__restrict__ ckpt, const bf16_t *__restrict__ out,
@@ -483,6 +493,7 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
     const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m);
     const bool active = n0 < g.N;
     bf16x8 Q[2][K / 16], D[2][K / 16];
+    float L;            // LSE in base 2 of row `lane`
     {
         // delta of the wave's rows: LP lanes share one
         const Rows os = grid_rows(g, pl, out, g.C), ds = grid_rows(g, pl, dout, g.C);
@@ -512,19 +523,22 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
         }
         const int n = n0 + lane, nc = n < g.N ? n : g.N - 1;
         const float e = lse[(int64_t)pl.u * g.N + nc];
-        const float L = n >= g.N || e == -INFINITY ? kNoRow : e * kLog2e;
-        const uint32_t wl = L == kNoRow ? pack_bf16(-kNoRow, 0.f) : split_bf16(-L), wd = split_bf16(-delta);
+        const bool none = n >= g.N || e == -INFINITY;
+        const uint32_t wl = none ? pack_bf16(-kNoRow, 0.f) : split_bf16(-e * bi.bs), wd = split_bf16(-delta);
+        L = none ? kNoRow : e * kLog2e;
         if (n < g.N) ext[(int64_t)pl.u * g.N + n] = uint2{wl, wd};
         bf16_t *area = S + wave * 64 * (K + 8);
         const Rows qs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 0) : grid_rows(g, pl, q, g.tstride);
-        stationary_rows<K, LP, SRC>(g, pl.win, qs, n0, area, Q, FixPair<K>{g.scale_c * kLog2e, wl});
-        stationary_rows<K, LP, SG>(g, pl.win, ds, n0, area, D, FixPair<K>{0.f, wd});
+        stationary_rows<K, LP, SRC>(g, pl.win, qs, n0, area, Q, FixScale{bi.qs});
+        stationary_rows<K, LP, SG>(g, pl.win, ds, n0, area, D, FixPair<K>{wd});
     }
     int mylin[2];
+    float mylse[2];
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
         const int n = n0 + qb * 32 + col;
         mylin[qb] = lin(g, n < g.N ? n : g.N - 1);
+        mylse[qb] = __shfl(L, qb * 32 + col);
     }
     // (the wave's own last window row, for its histogram)
     const int wsy1 = row_of(n0 + 63 < g.N ? n0 + 63 : g.N - 1, g.inv_m);
@@ -547,13 +561,16 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
     mv.request(g, pl.win, ks, vs, nullptr, 0);
     mv.template commit<K, K, true, ALN>(g, S, 0, 1.f);
     mv.request(g, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
+    f32x16 next, held;      // (CARRY) the bias of block (1, the coming one); dS of block (0, the last one)
+    if (CARRY && HIST) held = z;
     int before = -1;            // last streamed row of the chunk before
     for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
         const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
         const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
-        stage_bias<-1>(g, bi, ch, pl.hd, kLog2e, B, NT);
+        stage_bias<-1>(g, bi, ch, pl.hd, bi.bs, B, NT);
         double *const mine = H + wave * hsize + ch.c0 - (sy1 - wsy1) * bi.w2;
         __syncthreads();
+        if (CARRY && t0 == 0 && active) next = bias_block<ALN>(B + ch.c0 - mylin[1], words_of<ALN>(g, nullptr, 0, 0, hf));
         for (int tile = t0; tile < t1; ++tile) {
             const bf16_t *cur = S + (tile & 1) * I::STAGE;
             if (tile + 1 < ntiles) {
@@ -574,21 +591,20 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
 #pragma unroll
                         for (int i = 0; i < 2; ++i) At[db][i] = read_tr<I::XS>(cur + (kb * 32 + 16 * i) * I::XS, tro, 32 * db);
 #pragma unroll
-                    for (int qb = 0; qb < 2; ++qb) {
-                        f32x16 s = bias_block<ALN>(B + ch.c0 - mylin[qb], wd), p = z;
+                    for (int qx = 0; qx < 2; ++qx) {
+                        const int qb = 1 - qx;
+                        f32x16 s = CARRY && qb == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[qb], wd), p = z;
+                        if (CARRY && qb == 0) next = s;
 #pragma unroll
                         for (int i = 0; i < K / 16; ++i) s = mfma(Ak[i], Q[qb][i], s);
 #pragma unroll
                         for (int i = 0; i < K / 16; ++i) p = mfma(Av[i], D[qb][i], p);
                         if (!ALN) mask_rows(s, key0, g.N, hf);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]) * p[i];
-                        if (HIST) {
-                            double *const h = mine - mylin[qb];
-#pragma unroll
-                            for (int i = 0; i < 16; ++i)
-                                __hip_atomic_fetch_add(h + wd(i), (double)s[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                        }
+                        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], bi.c, -mylse[qb])) * p[i];
+                        if (HIST && CARRY && qb == 1) add_offsets<ALN>(mine - mylin[1], wd, s + held);
+                        else if (HIST && CARRY) held = s;
+                        else if (HIST) add_offsets<ALN>(mine - mylin[qb], wd, s);
                         uint32_t P[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) P[i] = pack_bf16(s[2 * i], s[2 * i + 1]);
@@ -603,6 +619,10 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
             __syncthreads();
         }
         if (HIST) {
+            if (CARRY && t1 == ntiles) {
+                if (active) add_offsets<ALN>(mine - mylin[0], words_of<ALN>(g, nullptr, ntiles - 1, 1, hf), held);
+                __syncthreads();
+            }
             flush<W, 64>(g, bi, ch, H, hsize, first, sy0, sy1, before,
                          part + ((int64_t)pl.u * nblk + pl.blk) * prows * bi.w2 + ch.ty0 * bi.w2);
             before = ch.ty1;
@@ -620,7 +640,7 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
 
 // ---- backward: dk, dv --------------------------------------------------------------------------------------------
 
-template <int K, int DB, int SRC, int SG, bool ALN, int W>
+template <int K, int DB, int SRC, int SG, bool ALN, bool CARRY, int W>
 __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias bi, int nblk, const bf16_t *__restrict__ q,
                                                         const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
                                                         const uint8_t *__restrict__ ckpt, const bf16_t *__restrict__ dout,
@@ -643,8 +663,8 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
         bf16_t *area = S + wave * 64 * (K + 8);
         const Rows ks = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 1) : grid_rows(g, pl, k, g.tstride);
         const Rows vs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 2) : grid_rows(g, pl, v, g.tstride);
-        stationary_rows<K, LP, SRC>(g, pl.win, ks, n0, area, Kb, FixPair<K>{0.f, kOnes});
-        stationary_rows<K, LP, SRC>(g, pl.win, vs, n0, area, Vb, FixPair<K>{0.f, kOnes});
+        stationary_rows<K, LP, SRC>(g, pl.win, ks, n0, area, Kb, FixPair<K>{kOnes});
+        stationary_rows<K, LP, SRC>(g, pl.win, vs, n0, area, Vb, FixPair<K>{kOnes});
     }
     int mylin[2];
 #pragma unroll
@@ -666,8 +686,9 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
             for (int i = 0; i < 16; ++i) Ak[b][db][i] = 0.f, Av[b][db][i] = 0.f;
     const int ntiles = (g.N + kTile - 1) / kTile;
     const int tro = tr_lane_offset<I::XS>(lane), ako = col * I::XS + 8 * hf;
-    const float scale = g.scale_c * kLog2e;
+    const float scale = bi.qs;
     const f32x16 z = {0};
+    f32x16 next;            // (CARRY) the bias of block (1, the coming one)
     Mover<LP, W, SRC, SG, true> mv;
     mv.request(g, pl.win, qs, ds, ex, 0);
     mv.template commit<K, K, false, ALN>(g, S, 0, scale);
@@ -675,8 +696,9 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
     for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
         const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
         const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
-        stage_bias<1>(g, bi, ch, pl.hd, kLog2e, B, NT);
+        stage_bias<1>(g, bi, ch, pl.hd, bi.bs, B, NT);
         __syncthreads();
+        if (CARRY && t0 == 0 && active) next = bias_block<ALN>(B + ch.c0 - mylin[1], words_of<ALN>(g, nullptr, 0, 0, hf));
         for (int tile = t0; tile < t1; ++tile) {
             const bf16_t *cur = S + (tile & 1) * I::STAGE;
             if (tile + 1 < ntiles) {
@@ -699,15 +721,17 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
                             Td[db][i] = read_tr<I::YS>(cur + I::YR + (qb * 32 + 16 * i) * I::YS, tro, 32 * db);
                         }
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        f32x16 s = bias_block<ALN>(B + ch.c0 - mylin[b], wd), p = z;
+                    for (int bx = 0; bx < 2; ++bx) {
+                        const int b = 1 - bx;
+                        f32x16 s = CARRY && b == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[b], wd), p = z;
+                        if (CARRY && b == 0) next = s;
 #pragma unroll
                         for (int i = 0; i < K / 16; ++i) s = mfma(Aq[i], Kb[b][i], s);
 #pragma unroll
                         for (int i = 0; i < K / 16; ++i) p = mfma(Ad[i], Vb[b][i], p);
                         uint32_t P[8], G[8];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]);
+                        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * bi.c);
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             P[i] = pack_bf16(s[2 * i], s[2 * i + 1]);
@@ -733,7 +757,7 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
         const int64_t at = (pl.img + pixel(pl.win, n)) * g.C + pl.hd * g.d;
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
-            store_row<SG>(dk + at, Ak[b][db], db, g.d, hf, kLn2);       // (Q carries scale * log2 e)
+            store_row<SG>(dk + at, Ak[b][db], db, g.d, hf, bi.ks);
             store_row<SG>(dv + at, Av[b][db], db, g.d, hf, 1.f);
         }
     }
@@ -743,15 +767,20 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
 
 constexpr size_t kBiasBytes = 36 * 1024, kHistBytes = 9 * 1024;
 
-template <int KX, int DB, bool SUM, int SRC, bool ALN, int W>
+// Whether the offsets of block (b + 1, t + 1), of stationary and streamed blocks of 32, are those of (b, t), lane by lane: 32 tokens on is whole
+// window rows on for both.  A wave then carries what belongs to a block's offsets over to the next step.
+inline bool carries(const Geo &g) { return g.M == 32 || g.M == 16; }
+
+template <int KX, int DB, bool SUM, int SRC, bool ALN, bool CARRY, int W>
 hipError_t launch_fwd_one(const Geo &g, const FwdArgs &a)
 {
-    Bias bi{a.bias, 0, 0, 0, 0};
+    Bias bi{a.bias};
+    plan_scale(g, &bi);
     plan_chunks(g, RIB_BF16, &bi, false, kBiasBytes, 0);
     const int nblk = (g.N + 64 * W - 1) / (64 * W);
     const size_t smem = stage_bytes<KX, 32 * DB, W>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.w2 * 4;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
-    auto kern = fwd_kernel<KX, DB, SUM, SRC, ALN, W>;
+    auto kern = fwd_kernel<KX, DB, SUM, SRC, ALN, CARRY, W>;
     const hipError_t e = prepare_kernel((const void *)kern, nullptr);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * nblk)), dim3(64 * W), smem, a.st, g, bi, nblk, a.force_max, (const bf16_t *)a.q,
@@ -761,19 +790,23 @@ hipError_t launch_fwd_one(const Geo &g, const FwdArgs &a)
 template <int KX, int DB, bool SUM, int SRC>
 hipError_t launch_fwd_src(const Geo &g, const FwdArgs &a)
 {
-    if (g.N <= 64) return launch_fwd_one<KX, DB, SUM, SRC, false, 1>(g, a);
-    if (SRC == kFast && g.M % 8 == 0) return launch_fwd_one<KX, DB, SUM, SRC, SRC == kFast, 4>(g, a);
-    return launch_fwd_one<KX, DB, SUM, SRC, false, 4>(g, a);
+    if (g.N <= 64) return launch_fwd_one<KX, DB, SUM, SRC, false, false, 1>(g, a);
+    if constexpr (SRC == kFast) {
+        if (carries(g)) return launch_fwd_one<KX, DB, SUM, SRC, true, true, 4>(g, a);
+        if (g.M % 8 == 0) return launch_fwd_one<KX, DB, SUM, SRC, true, false, 4>(g, a);
+    }
+    return launch_fwd_one<KX, DB, SUM, SRC, false, false, 4>(g, a);
 }
 
-template <int K, int DB, int SRC, int SG, bool ALN, int W, bool HIST>
+template <int K, int DB, int SRC, int SG, bool ALN, bool CARRY, int W, bool HIST>
 hipError_t launch_dq_one(const Geo &g, const BwdArgs &a, const Ws &ws)
 {
-    Bias bi{a.bias, 0, 0, 0, 0};
+    Bias bi{a.bias};
+    plan_scale(g, &bi);
     plan_chunks(g, RIB_BF16, &bi, HIST, kBiasBytes, kHistBytes);
     const size_t smem = stage_bytes<K, K, W>() + 8 * (size_t)g.M + ((size_t)bi.rows * bi.w2 + 1) / 2 * 8 + (size_t)W * bi.hrows * bi.w2 * 8;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
-    auto kern = dq_kernel<K, DB, SRC, SG, ALN, W, HIST>;
+    auto kern = dq_kernel<K, DB, SRC, SG, ALN, CARRY, W, HIST>;
     const hipError_t e = prepare_kernel((const void *)kern, nullptr);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * ws.nblk)), dim3(64 * W), smem, a.st, g, bi, ws.nblk, ws.prows, (const bf16_t *)a.q,
@@ -781,16 +814,17 @@ hipError_t launch_dq_one(const Geo &g, const BwdArgs &a, const Ws &ws)
                        (bf16_t *)a.dq, (uint2 *)((char *)a.ws + ws.ext), (float *)((char *)a.ws + ws.part));
     return hipGetLastError();
 }
-template <int K, int DB, int SRC, int SG, bool ALN, int W>
+template <int K, int DB, int SRC, int SG, bool ALN, bool CARRY, int W>
 hipError_t launch_pair(const Geo &g, const BwdArgs &a, const Ws &ws)
 {
-    hipError_t e = a.dbias != nullptr ? launch_dq_one<K, DB, SRC, SG, ALN, W, true>(g, a, ws) : launch_dq_one<K, DB, SRC, SG, ALN, W, false>(g, a, ws);
+    hipError_t e = a.dbias != nullptr ? launch_dq_one<K, DB, SRC, SG, ALN, CARRY, W, true>(g, a, ws) : launch_dq_one<K, DB, SRC, SG, ALN, CARRY, W, false>(g, a, ws);
     if (e != hipSuccess) return e;
-    Bias bi{a.bias, 0, 0, 0, 0};
+    Bias bi{a.bias};
+    plan_scale(g, &bi);
     plan_chunks(g, RIB_BF16, &bi, false, kBiasBytes, 0);
     const size_t smem = stage_bytes<K, K, W>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.w2 * 4;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
-    auto kern = dkv_kernel<K, DB, SRC, SG, ALN, W>;
+    auto kern = dkv_kernel<K, DB, SRC, SG, ALN, CARRY, W>;
     e = prepare_kernel((const void *)kern, nullptr);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * ws.nblk)), dim3(64 * W), smem, a.st, g, bi, ws.nblk, (const bf16_t *)a.q,
@@ -801,9 +835,12 @@ hipError_t launch_pair(const Geo &g, const BwdArgs &a, const Ws &ws)
 template <int K, int DB, int SRC, int SG>
 hipError_t launch_bwd_src(const Geo &g, const BwdArgs &a, const Ws &ws)
 {
-    if (g.N <= 64) return launch_pair<K, DB, SRC, SG, false, 1>(g, a, ws);
-    if (SG == kFast && g.M % 8 == 0) return launch_pair<K, DB, SRC, SG, SG == kFast, 4>(g, a, ws);
-    return launch_pair<K, DB, SRC, SG, false, 4>(g, a, ws);
+    if (g.N <= 64) return launch_pair<K, DB, SRC, SG, false, false, 1>(g, a, ws);
+    if constexpr (SG == kFast) {
+        if (carries(g)) return launch_pair<K, DB, SRC, SG, true, true, 4>(g, a, ws);
+        if (g.M % 8 == 0) return launch_pair<K, DB, SRC, SG, true, false, 4>(g, a, ws);
+    }
+    return launch_pair<K, DB, SRC, SG, false, false, 4>(g, a, ws);
 }
 template <int K, int DB, int SG>
 hipError_t launch_bwd(const Geo &g, const BwdArgs &a, const Ws &ws)

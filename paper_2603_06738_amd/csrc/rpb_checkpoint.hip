@@ -10,86 +10,137 @@ namespace rib {
 namespace rpb {
 namespace {
 
-__device__ __forceinline__ float load(const float *p) { return *p; }
-__device__ __forceinline__ float load(const bf16_t *p) { return widen(*p); }
+// A workgroup takes 32 tokens of a window, head after head: LP lanes a row, 8 values each, so that the rows it writes of a head
+// lie in one piece, and the heads' reads of a pixel come from the same lines.
+constexpr int kTokens = 32;
+struct __attribute__((packed, aligned(4))) words4 {
+    uint32_t w[4];
+};
+struct Slot {
+    int hd, n, c;           // head, token of the window (-1: none), first value
+    int64_t row, at;        // row of the checkpoint within a tensor; element of the grid
+};
+template <int LP>
+__device__ __forceinline__ Slot slot_of(const Geo &g, int slot)
+{
+    Slot s;
+    const int chunks = (g.N + kTokens - 1) / kTokens, w = blockIdx.x / chunks, n = (blockIdx.x - w * chunks) * kTokens + (slot / LP) % kTokens;
+    s.hd = slot / (LP * kTokens), s.n = n < g.N ? n : -1, s.c = 8 * (slot % LP);
+    s.row = ((int64_t)w * g.heads + s.hd) * g.N + n;
+    s.at = s.n < 0 ? 0 : grid_token(g, w, n) * g.tstride + (int64_t)s.hd * g.d;
+    return s;
+}
+// Values c .. c+7 of a row, zeros past its end.
+template <bool PAIRS>
+__device__ __forceinline__ void load8(const bf16_t *p, int c, int d, float (&x)[8])
+{
+    if (PAIRS && c + 8 <= d) {
+        const words4 v = *(const words4 *)(p + c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(i & 1 ? v.w[i >> 1] & 0xffff0000u : v.w[i >> 1] << 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = c + i < d ? widen(p[c + i]) : 0.f;
+    }
+}
+template <bool PAIRS>
+__device__ __forceinline__ void load8(const float *p, int c, int d, float (&x)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = c + i < d ? p[c + i] : 0.f;
+}
 
-// 16 lanes a row, 4 values each.
-template <class T>
+template <class T, int LP, bool PAIRS>
 __global__ __launch_bounds__(256) void pack_kernel(Geo g, const T *__restrict__ q, const T *__restrict__ k, const T *__restrict__ v,
                                                    uint8_t *__restrict__ ckpt)
 {
-    const int64_t rows = g.units * g.N, row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
-    if (row >= rows) return;
-    const int dp = ckpt_row(g.d), c = 4 * (threadIdx.x & 15), which = blockIdx.y;
-    // rows in the order token, head: neighbours share a pixel
-    const int64_t wt = row / g.heads;
-    const int hd = (int)(row - wt * g.heads), w = (int)(wt / g.N), n = (int)(wt - (int64_t)w * g.N);
-    const T *src = (which == 0 ? q : which == 1 ? k : v) + grid_token(g, w, n) * g.tstride + (int64_t)hd * g.d;
-    const int64_t to = ((int64_t)w * g.heads + hd) * g.N + n + which * rows;
-    float x[4];
-    uint32_t big = 0u;
+    const int dp = ckpt_row(g.d), which = blockIdx.y;
+    const int64_t rows = ckpt_rows(g);
+    const T *src = which == 0 ? q : which == 1 ? k : v;
+    for (int slot = threadIdx.x; slot < kTokens * LP * g.heads; slot += 256) {      // (the lanes of a row stay together)
+        const Slot s = slot_of<LP>(g, slot);
+        float x[8];
+        uint32_t big = 0u;
+        if (s.n >= 0) load8<PAIRS>(src + s.at, s.c, g.d, x);
+        else
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[i] = c + i < g.d ? load(src + c + i) : 0.f;
-        const uint32_t a = __float_as_uint(x[i]) & 0x7fffffffu;
-        big = a > big ? a : big;
-    }
+            for (int i = 0; i < 8; ++i) x[i] = 0.f;
 #pragma unroll
-    for (int m = 1; m < 16; m <<= 1) {
-        const uint32_t o = (uint32_t)__shfl_xor((int)big, m);
-        big = o > big ? o : big;
-    }
-    // big = 1.f 2^(E - 127): 127 steps of 2^(E - 127 - 6) hold it unless its fraction is above 127/64 - 1
-    int e = 0;
-    if (big >= 0x7f800000u) e = 255;                        // not finite: the row stands for NaN
-    else if (big != 0u) {
-        e = (int)(big >> 23) - 6 + ((big & 0x7fffffu) > 0x7e0000u ? 1 : 0);
-        if (e < 1) e = 1;
-    }
-    uint32_t codes = 0u;
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t a = __float_as_uint(x[i]) & 0x7fffffffu;
+            big = a > big ? a : big;
+        }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int s = e == 0 || e == 255 ? 0 : (int)rintf(ldexpf(x[i], 127 - e));
-        codes |= (uint32_t)(s + 128) << (8 * i);
+        for (int m = 1; m < LP; m <<= 1) {
+            const uint32_t o = (uint32_t)__shfl_xor((int)big, m);
+            big = o > big ? o : big;
+        }
+        // big = 1.f 2^(E - 127): 127 steps of 2^(E - 127 - 6) hold it unless its fraction is above 127/64 - 1
+        int e = 0;
+        if (big >= 0x7f800000u) e = 255;                        // not finite: the row stands for NaN
+        else if (big != 0u) {
+            e = (int)(big >> 23) - 6 + ((big & 0x7fffffu) > 0x7e0000u ? 1 : 0);
+            if (e < 1) e = 1;
+        }
+        const float per = e == 0 || e == 255 ? 0.f : __uint_as_float((uint32_t)(254 - e) << 23);
+        uint32_t codes[2] = {0u, 0u};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) codes[i >> 2] |= (uint32_t)((e == 255 ? 0 : (int)rintf(x[i] * per)) + 128) << (8 * (i & 3));
+        if (s.n < 0) continue;
+        const int64_t to = s.row + which * rows;
+        if (s.c < dp) *(uint2 *)(ckpt + to * dp + s.c) = uint2{codes[0], codes[1]};
+        if (s.c == 0) (ckpt + 3 * rows * dp)[to] = (uint8_t)e;
     }
-    if (c < dp) *(uint32_t *)(ckpt + to * dp + c) = codes;
-    if (c == 0) (ckpt + 3 * rows * dp)[to] = (uint8_t)e;
 }
 
-template <class T>
+template <class T, int LP>
 __global__ __launch_bounds__(256) void unpack_kernel(Geo g, const uint8_t *__restrict__ ckpt, T *__restrict__ q, T *__restrict__ k, T *__restrict__ v)
 {
-    const int64_t rows = g.units * g.N, row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
-    if (row >= rows) return;
-    const int dp = ckpt_row(g.d), c = 4 * (threadIdx.x & 15), which = blockIdx.y;
-    const int64_t wt = row / g.heads;
-    const int hd = (int)(row - wt * g.heads), w = (int)(wt / g.N), n = (int)(wt - (int64_t)w * g.N);
-    T *dst = (which == 0 ? q : which == 1 ? k : v) + grid_token(g, w, n) * g.tstride + (int64_t)hd * g.d;
-    const int64_t from = ((int64_t)w * g.heads + hd) * g.N + n + which * rows;
-    const float s = __uint_as_float((uint32_t)(ckpt + 3 * rows * dp)[from] << 23), z = -128.f * s;
-    if (c >= g.d) return;
-    const uint32_t codes = *(const uint32_t *)(ckpt + from * dp + c);
+    const int dp = ckpt_row(g.d), which = blockIdx.y;
+    const int64_t rows = ckpt_rows(g);
+    T *dst = which == 0 ? q : which == 1 ? k : v;
+    for (int slot = threadIdx.x; slot < kTokens * LP * g.heads; slot += 256) {
+        const Slot s = slot_of<LP>(g, slot);
+        if (s.n < 0 || s.c >= g.d) continue;
+        const int64_t from = s.row + which * rows;
+        const float sc = __uint_as_float((uint32_t)(ckpt + 3 * rows * dp)[from] << 23), z = -128.f * sc;
+        const uint2 codes = *(const uint2 *)(ckpt + from * dp + s.c);
+        T *p = dst + s.at + s.c;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (c + i < g.d) store_as(dst + c + i, fmaf((float)((codes >> (8 * i)) & 255u), s, z));
+        for (int i = 0; i < 8; ++i)
+            if (s.c + i < g.d) store_as(p + i, fmaf((float)(((i < 4 ? codes.x : codes.y) >> (8 * (i & 3))) & 255u), sc, z));
+    }
 }
 
 }  // namespace
 
+template <class T, int LP>
+hipError_t pack_width(const Geo &g, bool pairs, const void *q, const void *k, const void *v, uint8_t *ckpt, hipStream_t st)
+{
+    const dim3 grid((unsigned)(g.units / g.heads * ((g.N + kTokens - 1) / kTokens)), 3);
+    if (pairs) hipLaunchKernelGGL((pack_kernel<T, LP, true>), grid, dim3(256), 0, st, g, (const T *)q, (const T *)k, (const T *)v, ckpt);
+    else hipLaunchKernelGGL((pack_kernel<T, LP, false>), grid, dim3(256), 0, st, g, (const T *)q, (const T *)k, (const T *)v, ckpt);
+    return hipGetLastError();
+}
+template <class T>
+hipError_t unpack_type(const Geo &g, const uint8_t *ckpt, void *q, void *k, void *v, hipStream_t st)
+{
+    const dim3 grid((unsigned)(g.units / g.heads * ((g.N + kTokens - 1) / kTokens)), 3);
+    if (g.d <= 32) hipLaunchKernelGGL((unpack_kernel<T, 4>), grid, dim3(256), 0, st, g, ckpt, (T *)q, (T *)k, (T *)v);
+    else hipLaunchKernelGGL((unpack_kernel<T, 8>), grid, dim3(256), 0, st, g, ckpt, (T *)q, (T *)k, (T *)v);
+    return hipGetLastError();
+}
+
 hipError_t launch_pack(const Geo &g, int dtype, const void *q, const void *k, const void *v, uint8_t *ckpt, hipStream_t st)
 {
-    const dim3 grid((unsigned)((g.units * g.N + 15) / 16), 3);
-    if (dtype == RIB_BF16)
-        hipLaunchKernelGGL(pack_kernel<bf16_t>, grid, dim3(256), 0, st, g, (const bf16_t *)q, (const bf16_t *)k, (const bf16_t *)v, ckpt);
-    else hipLaunchKernelGGL(pack_kernel<float>, grid, dim3(256), 0, st, g, (const float *)q, (const float *)k, (const float *)v, ckpt);
-    return hipGetLastError();
+    if (dtype != RIB_BF16)
+        return g.d <= 32 ? pack_width<float, 4>(g, false, q, k, v, ckpt, st) : pack_width<float, 8>(g, false, q, k, v, ckpt, st);
+    const bool pairs = !(g.d & 1) && !(g.tstride & 1) && (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v) & 3) == 0;
+    return g.d <= 32 ? pack_width<bf16_t, 4>(g, pairs, q, k, v, ckpt, st) : pack_width<bf16_t, 8>(g, pairs, q, k, v, ckpt, st);
 }
 hipError_t launch_unpack(const Geo &g, int dtype, const uint8_t *ckpt, void *q, void *k, void *v, hipStream_t st)
 {
-    const dim3 grid((unsigned)((g.units * g.N + 15) / 16), 3);
-    if (dtype == RIB_BF16) hipLaunchKernelGGL(unpack_kernel<bf16_t>, grid, dim3(256), 0, st, g, ckpt, (bf16_t *)q, (bf16_t *)k, (bf16_t *)v);
-    else hipLaunchKernelGGL(unpack_kernel<float>, grid, dim3(256), 0, st, g, ckpt, (float *)q, (float *)k, (float *)v);
-    return hipGetLastError();
+    return dtype == RIB_BF16 ? unpack_type<bf16_t>(g, ckpt, q, k, v, st) : unpack_type<float>(g, ckpt, q, k, v, st);
 }
 
 }  // namespace rpb

@@ -24,7 +24,20 @@ struct Bias {
     int chunk;              // tiles a chunk
     int rows;               // bias rows in LDS at most
     int hrows;              // rows of a wave's histogram at most
+    // Logits in the products' own unit, q.k + bias / scale: `qs` is what q is multiplied by first (1: as it is), `bs` the
+    // bias, and `c` brings a sum to base 2.  `ks`: what dS q is multiplied by.
+    float qs, bs, c, ks;
 };
+// Scales that are no ordinary positive number go into q (rounded to its type), so that neither bias / scale nor
+// an excluded pair's minus infinity comes out wrong.
+inline void plan_scale(const Geo &g, Bias *b)
+{
+    const bool plain = g.scale_c >= 0x1p-40f && g.scale_c <= 0x1p40f;
+    b->qs = plain ? 1.f : g.scale_c;
+    b->bs = plain ? 1.f / g.scale_c : 1.f;
+    b->c = plain ? g.scale_c * rows::kLog2e : rows::kLog2e;
+    b->ks = plain ? g.scale_c : 1.f;
+}
 
 // The most window rows that `len` tokens from a multiple of `len` on touch.
 inline int most_rows(int len, int N, int M)
@@ -50,6 +63,26 @@ __device__ __forceinline__ Chunk chunk_of(const Geo &g, const Bias &b, int t0, i
     return c;
 }
 __device__ __forceinline__ int lin(const Geo &g, int n) { return n + row_of(n, g.inv_m) * (g.M - 1); }
+
+// Whether some key is not excluded for query n; asked by whole waves.
+__device__ __forceinline__ bool has_key(const Geo &g, const Bias &b, int hd, int n)
+{
+    const float *row = b.bias + (int64_t)hd * b.w2 * b.w2 + 2 * g.M * (g.M - 1) + lin(g, n);
+    for (int j0 = 0; j0 < g.N; j0 += 64) {
+        const int j = j0 + (threadIdx.x & 63);
+        if (__any(j < g.N && !(row[-lin(g, j < g.N ? j : 0)] <= kExcluded))) return true;
+    }
+    return false;
+}
+// Whether a wave's walk without a running maximum has to be done again: a denominator that left [2^-60, 2^60], other than
+// zeros of rows without a key.  `n`: the lane's row, the same in both halves.
+__device__ __forceinline__ bool bad_rows(const Geo &g, const Bias &b, int hd, int n, float sum)
+{
+    if (__any(!(sum >= 0x1p-60f && sum <= 0x1p60f) && sum != 0.f)) return true;
+    for (uint32_t zeros = (uint32_t)__ballot(sum == 0.f && n < g.N); zeros != 0u; zeros &= zeros - 1u)
+        if (has_key(g, b, hd, __shfl(n, __ffs((int)zeros) - 1))) return true;
+    return false;
+}
 
 // Copies a chunk's bias rows to LDS, times `scale`; excluded pairs as minus infinity.  SGN = -1: the streamed tokens are the keys
 // (offset = query - key falls as the key rises), +1: the queries.

@@ -184,7 +184,7 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
     for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
         const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
         const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
-        stage_bias<-1>(g, bi, ch, pl.hd, kLog2e, B, NT);
+        stage_bias<-1>(g, bi, ch, pl.hd, 1.f, B, NT);
         __syncthreads();
         for (int tile = t0; tile < t1; ++tile) {
             const float *cur = S + (tile & 1) * I::STAGE;
@@ -200,6 +200,8 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
                     const Words16<ALN> wd = words_of<ALN>(g, (const int *)(cur + I::LT), tile, kb, hf);
                     f32x16 s = scores<DB>(cur + (kb * 32 + col) * I::STR + 4 * hf, Q, bias_block<ALN>(B + ch.c0 - mylin, wd), g.d);
                     if (!ALN) mask_rows(s, key0, g.N, hf);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] *= kLog2e;
                     if (MAX) {
                         float m = s[0];
 #pragma unroll
@@ -248,15 +250,16 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void fwd_kernel(Geo g, Bias
     const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m), nc = n < g.N ? n : g.N - 1;
     const bool active = n0 < g.N;
     Raw Q[4 * DB];
-    operand<DB, false>(g, pl, rows_of_grid(g, pl, q, g.tstride), nc, g.scale_c * kLog2e, Q);
+    operand<DB, false>(g, pl, rows_of_grid(g, pl, q, g.tstride), nc, g.scale_c, Q);
     const Rows ks = rows_of_grid(g, pl, k, g.tstride), vs = rows_of_grid(g, pl, v, g.tstride);
     f32x16 O[DB];
     float sum, top;
-    // First without a running maximum; a denominator outside [2^-60, 2^60] sends the workgroup on a second walk, with one.
+    // First without a running maximum; a denominator outside [2^-60, 2^60], and not for want of keys, sends the
+    // workgroup on a second walk, with one.
     bool bad = true;
     if (!force_max) {
         fwd_walk<false, DB, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, sy0, sy1, lin(g, nc), active);
-        bad = active && !((sum >= 0x1p-60f) && (sum <= 0x1p60f));
+        bad = active && bad_rows(g, bi, pl.hd, n, sum);
     }
     if (__syncthreads_or(bad)) fwd_walk<true, DB, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, sy0, sy1, lin(g, nc), active);
     if (n >= g.N) return;
@@ -265,7 +268,7 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void fwd_kernel(Geo g, Bias
     store_row<DB>(out + (pl.img + pixel(pl.win, n)) * g.C + pl.hd * g.d, O, g.d, hf, inv);
 }
 
-// dq and the bias's gradient; the second kernel's -LSE * log2 e and -delta of every row.
+// dq and the bias's gradient; the second kernel's -LSE and -delta of every row.
 template <int DB, bool CKPT, bool ALN, int W, bool HIST>
 __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias bi, int nblk, int prows, const float *__restrict__ q,
                                                        const float *__restrict__ k, const float *__restrict__ v,
@@ -299,8 +302,8 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
         for (int i = 0; i < 4 * DB; ++i) delta += (O[i].x * D[i].x + O[i].y * D[i].y) + (O[i].z * D[i].z + O[i].w * D[i].w);
         delta += __shfl_xor(delta, 32);
     }
-    operand<DB, CKPT>(g, pl, CKPT ? rows_of_ckpt(g, pl, ckpt, 0) : rows_of_grid(g, pl, q, g.tstride), nc, g.scale_c * kLog2e, Q);
-    const float e0 = lse[(int64_t)pl.u * g.N + nc], L = n >= g.N || e0 == -INFINITY ? bf::kNoRow : e0 * kLog2e;
+    operand<DB, CKPT>(g, pl, CKPT ? rows_of_ckpt(g, pl, ckpt, 0) : rows_of_grid(g, pl, q, g.tstride), nc, g.scale_c, Q);
+    const float e0 = lse[(int64_t)pl.u * g.N + nc], L = n >= g.N || e0 == -INFINITY ? bf::kNoRow : e0;
     if (n < g.N && hf == 0) ext[(int64_t)pl.u * g.N + n] = float2{-L, -delta};
     const int mylin = lin(g, nc), wsy1 = row_of(n0 + 31 < g.N ? n0 + 31 : g.N - 1, g.inv_m);
     const Rows ks = CKPT ? rows_of_ckpt(g, pl, ckpt, 1) : rows_of_grid(g, pl, k, g.tstride);
@@ -320,7 +323,7 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
     for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
         const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
         const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
-        stage_bias<-1>(g, bi, ch, pl.hd, kLog2e, B, NT);
+        stage_bias<-1>(g, bi, ch, pl.hd, 1.f, B, NT);
         double *const mine = H + wave * hsize + ch.c0 - (sy1 - wsy1) * bi.w2 - mylin;
         __syncthreads();
         for (int tile = t0; tile < t1; ++tile) {
@@ -340,7 +343,7 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
                     const f32x16 p = scores<DB>(row + I::YR, D, z, g.d);
                     if (!ALN) mask_rows(s, key0, g.N, hf);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] - L) * (p[i] - delta);
+                    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f((s[i] - L) * kLog2e) * (p[i] - delta);
                     if (HIST) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
@@ -391,7 +394,8 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
 #pragma unroll
         for (int i = 0; i < 16; ++i) Ak[db][i] = 0.f, Av[db][i] = 0.f;
     const int ntiles = (g.N + kTile - 1) / kTile;
-    const float scale = g.scale_c * kLog2e;
+    const float scale = g.scale_c;
+    const f32x16 z = {0};
     Mover<DB, W, CKPT, false, true> mv;
     mv.request(g, pl.win, qs, ds, ex, 0);
     mv.commit(g, S, 0, scale);
@@ -399,7 +403,7 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
     for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
         const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
         const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
-        stage_bias<1>(g, bi, ch, pl.hd, kLog2e, B, NT);
+        stage_bias<1>(g, bi, ch, pl.hd, 1.f, B, NT);
         __syncthreads();
         for (int tile = t0; tile < t1; ++tile) {
             const float *cur = S + (tile & 1) * I::STAGE;
@@ -413,19 +417,17 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
                     if (!ALN && tile * kTile + qb * 32 >= g.N) break;
                     const Words16<ALN> wd = words_of<ALN>(g, (const int *)(cur + I::LT), tile, qb, hf);
                     const float *row = cur + (qb * 32 + col) * I::STR + 4 * hf;
-                    f32x16 s = bias_block<ALN>(B + ch.c0 - mylin, wd), p;
+                    f32x16 s = scores<DB>(row, Kb, bias_block<ALN>(B + ch.c0 - mylin, wd), g.d), p = scores<DB>(row + I::YR, Vb, z, g.d);
+                    // (LSE and delta only then: sums that start from them would round at their size)
 #pragma unroll
                     for (int a = 0; a < 4; ++a) {
                         const float4 l = *(const float4 *)(cur + I::EX + qb * 32 + 8 * a + 4 * hf), dl = *(const float4 *)(cur + I::EX + kTile + qb * 32 + 8 * a + 4 * hf);
-                        s[4 * a] += l.x, s[4 * a + 1] += l.y, s[4 * a + 2] += l.z, s[4 * a + 3] += l.w;
-                        p[4 * a] = dl.x, p[4 * a + 1] = dl.y, p[4 * a + 2] = dl.z, p[4 * a + 3] = dl.w;
-                    }
-                    s = scores<DB>(row, Kb, s, g.d);
-                    p = scores<DB>(row + I::YR, Vb, p, g.d);
+                        const float lr[4] = {l.x, l.y, l.z, l.w}, dr[4] = {dl.x, dl.y, dl.z, dl.w};
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        s[i] = __builtin_amdgcn_exp2f(s[i]);
-                        p[i] *= s[i];
+                        for (int r = 0; r < 4; ++r) {
+                            s[4 * a + r] = __builtin_amdgcn_exp2f((s[4 * a + r] + lr[r]) * kLog2e);
+                            p[4 * a + r] = (p[4 * a + r] + dr[r]) * s[4 * a + r];
+                        }
                     }
                     contract<DB>(Av, cur + I::YR + (qb * 32 + 4 * hf) * I::STR + col, s);
                     contract<DB>(Ak, cur + (qb * 32 + 4 * hf) * I::STR + col, p);
@@ -436,7 +438,7 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
     }
     if (n >= g.N) return;
     const int64_t at = (pl.img + pixel(pl.win, n)) * g.C + pl.hd * g.d;
-    store_row<DB>(dk + at, Ak, g.d, hf, kLn2);          // (Q carries scale * log2 e)
+    store_row<DB>(dk + at, Ak, g.d, hf, 1.f);           // (Q carries the scale)
     store_row<DB>(dv + at, Av, g.d, hf, 1.f);
 }
 
@@ -445,7 +447,7 @@ constexpr size_t kBiasBytes = 36 * 1024, kHistBytes = 9 * 1024;
 template <int DB, bool ALN, int W>
 hipError_t launch_fwd_one(const Geo &g, const FwdArgs &a)
 {
-    Bias bi{a.bias, 0, 0, 0, 0};
+    Bias bi{a.bias};
     plan_chunks(g, RIB_F32, &bi, false, kBiasBytes, 0);
     const int nblk = (g.N + 32 * W - 1) / (32 * W);
     const size_t smem = stage_bytes<DB>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.w2 * 4;
@@ -467,7 +469,7 @@ hipError_t launch_fwd_width(const Geo &g, const FwdArgs &a)
 template <int DB, bool CKPT, bool ALN, int W, bool HIST>
 hipError_t launch_dq_one(const Geo &g, const BwdArgs &a, const Ws &ws)
 {
-    Bias bi{a.bias, 0, 0, 0, 0};
+    Bias bi{a.bias};
     plan_chunks(g, RIB_F32, &bi, HIST, kBiasBytes, kHistBytes);
     const size_t smem = stage_bytes<DB>() + 8 * (size_t)g.M + ((size_t)bi.rows * bi.w2 + 1) / 2 * 8 + (size_t)W * bi.hrows * bi.w2 * 8;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
@@ -484,7 +486,7 @@ hipError_t launch_pair(const Geo &g, const BwdArgs &a, const Ws &ws)
 {
     hipError_t e = a.dbias != nullptr ? launch_dq_one<DB, CKPT, ALN, W, true>(g, a, ws) : launch_dq_one<DB, CKPT, ALN, W, false>(g, a, ws);
     if (e != hipSuccess) return e;
-    Bias bi{a.bias, 0, 0, 0, 0};
+    Bias bi{a.bias};
     plan_chunks(g, RIB_F32, &bi, false, kBiasBytes, 0);
     const size_t smem = stage_bytes<DB>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.w2 * 4;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;

@@ -122,3 +122,10 @@ def test_bucket_maps(dtype, M, kind):
         assert torch.isinf(c.lse[:, :, 0]).all()
     if kind == "none":
         assert (c.out == 0).all() and (c.dq == 0).all() and (c.dk == 0).all() and (c.dv == 0).all() and (c.dbias == 0).all()
+
+
+@pytest.mark.parametrize("dtype,M,heads,d", [("bf16", 32, 2, 30), ("bf16", 40, 1, 30), ("bf16", 48, 1, 32), ("bf16", 64, 1, 16), ("bf16", 37, 1, 20),
+                                             ("f32", 32, 1, 30), ("f32", 33, 1, 16), ("f32", 48, 1, 40), ("f32", 64, 1, 16)])
+def test_large_windows(dtype, M, heads, d):
+    """Several workgroups a unit; bias rows and sums in chunks of the walk."""
+    run(dtype, 1, M, M, heads, d, M, M // 3, seed=M)
