@@ -604,7 +604,7 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
                         for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], bi.c, -mylse[qb])) * p[i];
                         if (HIST && CARRY && qb == 1) add_offsets<ALN>(mine - mylin[1], wd, s + held);
                         else if (HIST && CARRY) held = s;
-                        else if (HIST) add_offsets<ALN>(mine - mylin[qb], wd, s);
+                        else if (HIST && (ALN || n0 + qb * 32 + col < g.N)) add_offsets<ALN>(mine - mylin[qb], wd, s);     // (many lanes at one word are slow)
                         uint32_t P[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) P[i] = pack_bf16(s[2 * i], s[2 * i + 1]);
@@ -787,17 +787,6 @@ hipError_t launch_fwd_one(const Geo &g, const FwdArgs &a)
                        (const bf16_t *)a.k, (const bf16_t *)a.v, (bf16_t *)a.out, a.lse);
     return hipGetLastError();
 }
-template <int KX, int DB, bool SUM, int SRC>
-hipError_t launch_fwd_src(const Geo &g, const FwdArgs &a)
-{
-    if (g.N <= 64) return launch_fwd_one<KX, DB, SUM, SRC, false, false, 1>(g, a);
-    if constexpr (SRC == kFast) {
-        if (carries(g)) return launch_fwd_one<KX, DB, SUM, SRC, true, true, 4>(g, a);
-        if (g.M % 8 == 0) return launch_fwd_one<KX, DB, SUM, SRC, true, false, 4>(g, a);
-    }
-    return launch_fwd_one<KX, DB, SUM, SRC, false, false, 4>(g, a);
-}
-
 template <int K, int DB, int SRC, int SG, bool ALN, bool CARRY, int W, bool HIST>
 hipError_t launch_dq_one(const Geo &g, const BwdArgs &a, const Ws &ws)
 {
@@ -832,30 +821,6 @@ hipError_t launch_pair(const Geo &g, const BwdArgs &a, const Ws &ws)
                        (bf16_t *)a.dk, (bf16_t *)a.dv);
     return hipGetLastError();
 }
-template <int K, int DB, int SRC, int SG>
-hipError_t launch_bwd_src(const Geo &g, const BwdArgs &a, const Ws &ws)
-{
-    if (g.N <= 64) return launch_pair<K, DB, SRC, SG, false, false, 1>(g, a, ws);
-    if constexpr (SG == kFast) {
-        if (carries(g)) return launch_pair<K, DB, SRC, SG, true, true, 4>(g, a, ws);
-        if (g.M % 8 == 0) return launch_pair<K, DB, SRC, SG, true, false, 4>(g, a, ws);
-    }
-    return launch_pair<K, DB, SRC, SG, false, false, 4>(g, a, ws);
-}
-template <int K, int DB, int SG>
-hipError_t launch_bwd(const Geo &g, const BwdArgs &a, const Ws &ws)
-{
-    return a.ckpt != nullptr ? launch_bwd_src<K, DB, kCkpt, SG>(g, a, ws) : launch_bwd_src<K, DB, SG, SG>(g, a, ws);
-}
-
-// One translation unit a width.
-hipError_t bwd32(const Geo &, const BwdArgs &, const Ws &);
-hipError_t bwd48(const Geo &, const BwdArgs &, const Ws &);
-hipError_t bwd48w(const Geo &, const BwdArgs &, const Ws &);
-hipError_t bwd64(const Geo &, const BwdArgs &, const Ws &);
-hipError_t bwd80(const Geo &, const BwdArgs &, const Ws &);
-hipError_t bwd_any(const Geo &, const BwdArgs &, const Ws &);
-
 }  // namespace bf
 }  // namespace rpb
 }  // namespace rib

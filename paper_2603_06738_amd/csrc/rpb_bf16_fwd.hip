@@ -1,7 +1,7 @@
 // Forward of the learned relative position bias, bf16, and the choice of the kernels' widths.
 #include <initializer_list>
 
-#include "rpb_bf16.h"
+#include "rpb_bf16_small.h"
 
 namespace rib {
 namespace rpb {
@@ -31,7 +31,7 @@ hipError_t launch_fwd_bf16(const Geo &g, const FwdArgs &a)
 
 hipError_t launch_bwd_bf16(const Geo &g, const BwdArgs &a)
 {
-    const Ws ws = ws_layout(g, RIB_BF16);
+    Ws ws = ws_layout(g, RIB_BF16);
     hipError_t e;
     if (!fast(g, {a.q, a.k, a.v, a.out, a.dout, a.dq, a.dk, a.dv})) e = bwd_any(g, a, ws);
     else if (g.d <= 30) e = bwd32(g, a, ws);        // two columns beside the head's for -LSE and -delta

@@ -10,8 +10,7 @@ namespace rib {
 namespace rpb {
 namespace {
 
-// A workgroup takes 32 tokens of a window, head after head: LP lanes a row, 8 values each, so that the rows it writes of a head
-// lie in one piece, and the heads' reads of a pixel come from the same lines.
+// A workgroup takes 32 tokens of a window, all heads of one after the other, LP lanes a row and 8 values a lane: a wave reads whole pixels.
 constexpr int kTokens = 32;
 struct __attribute__((packed, aligned(4))) words4 {
     uint32_t w[4];
@@ -20,14 +19,31 @@ struct Slot {
     int hd, n, c;           // head, token of the window (-1: none), first value
     int64_t row, at;        // row of the checkpoint within a tensor; element of the grid
 };
+// The workgroup's window and first token (all of it uniform).
+struct Corner {
+    int w, n0, y0, x0;
+    int64_t img;
+};
+__device__ __forceinline__ Corner corner_of(const Geo &g)
+{
+    Corner c;
+    const int chunks = (g.N + kTokens - 1) / kTokens;
+    c.w = blockIdx.x / chunks, c.n0 = (blockIdx.x - c.w * chunks) * kTokens;
+    const int wx = c.w % g.nwx, t = c.w / g.nwx, wy = t % g.nwy;
+    c.y0 = wy * g.M + g.s, c.x0 = wx * g.M + g.s, c.img = (int64_t)(t / g.nwy) * g.H * g.W;
+    return c;
+}
 template <int LP>
-__device__ __forceinline__ Slot slot_of(const Geo &g, int slot)
+__device__ __forceinline__ Slot slot_of(const Geo &g, const Corner &k, int slot)
 {
     Slot s;
-    const int chunks = (g.N + kTokens - 1) / kTokens, w = blockIdx.x / chunks, n = (blockIdx.x - w * chunks) * kTokens + (slot / LP) % kTokens;
-    s.hd = slot / (LP * kTokens), s.n = n < g.N ? n : -1, s.c = 8 * (slot % LP);
-    s.row = ((int64_t)w * g.heads + s.hd) * g.N + n;
-    s.at = s.n < 0 ? 0 : grid_token(g, w, n) * g.tstride + (int64_t)s.hd * g.d;
+    const int r = slot / LP, tk = r / g.heads, n = k.n0 + tk, iy = row_of(n, g.inv_m);
+    s.hd = r - tk * g.heads, s.n = n < g.N ? n : -1, s.c = 8 * (slot % LP);
+    s.row = ((int64_t)k.w * g.heads + s.hd) * g.N + n;
+    int y = k.y0 + iy, x = k.x0 + n - iy * g.M;
+    if (y >= g.H) y -= g.H;
+    if (x >= g.W) x -= g.W;
+    s.at = s.n < 0 ? 0 : (k.img + (int64_t)y * g.W + x) * g.tstride + s.hd * g.d;
     return s;
 }
 // Values c .. c+7 of a row, zeros past its end.
@@ -57,8 +73,9 @@ __global__ __launch_bounds__(256) void pack_kernel(Geo g, const T *__restrict__ 
     const int dp = ckpt_row(g.d), which = blockIdx.y;
     const int64_t rows = ckpt_rows(g);
     const T *src = which == 0 ? q : which == 1 ? k : v;
+    const Corner corner = corner_of(g);
     for (int slot = threadIdx.x; slot < kTokens * LP * g.heads; slot += 256) {      // (the lanes of a row stay together)
-        const Slot s = slot_of<LP>(g, slot);
+        const Slot s = slot_of<LP>(g, corner, slot);
         float x[8];
         uint32_t big = 0u;
         if (s.n >= 0) load8<PAIRS>(src + s.at, s.c, g.d, x);
@@ -99,8 +116,9 @@ __global__ __launch_bounds__(256) void unpack_kernel(Geo g, const uint8_t *__res
     const int dp = ckpt_row(g.d), which = blockIdx.y;
     const int64_t rows = ckpt_rows(g);
     T *dst = which == 0 ? q : which == 1 ? k : v;
+    const Corner corner = corner_of(g);
     for (int slot = threadIdx.x; slot < kTokens * LP * g.heads; slot += 256) {
-        const Slot s = slot_of<LP>(g, slot);
+        const Slot s = slot_of<LP>(g, corner, slot);
         if (s.n < 0 || s.c >= g.d) continue;
         const int64_t from = s.row + which * rows;
         const float sc = __uint_as_float((uint32_t)(ckpt + 3 * rows * dp)[from] << 23), z = -128.f * sc;

@@ -166,6 +166,7 @@ struct Ws {
     size_t ext, part, total;
     int nblk;                           // workgroups a unit
     int prows;                          // rows of a workgroup's sums
+    int shares;                         // sums a head: of windows, or of the runs of windows a wave takes
 };
 // Stationary tokens of a wave, and of a workgroup.
 constexpr int wave_tokens(int dtype) { return dtype == RIB_BF16 ? 64 : 32; }
@@ -177,6 +178,7 @@ inline Ws ws_layout(const Geo &g, int dtype)
     w.nblk = (g.N + sb - 1) / sb;
     w.prows = g.M - 1 + most_rows(sb, g.N, g.M);
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+    w.shares = (int)(g.units / g.heads);
     w.ext = 0;
     w.part = up((size_t)g.units * g.N * 8);
     w.total = w.part + up((size_t)g.units * w.nblk * w.prows * (2 * g.M - 1) * sizeof(float));

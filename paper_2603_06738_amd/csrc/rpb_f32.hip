@@ -344,7 +344,7 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
                     if (!ALN) mask_rows(s, key0, g.N, hf);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f((s[i] - L) * kLog2e) * (p[i] - delta);
-                    if (HIST) {
+                    if (HIST && (ALN || n < g.N)) {         // (many lanes at one word are slow)
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
                             __hip_atomic_fetch_add(mine + wd(i), (double)s[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);

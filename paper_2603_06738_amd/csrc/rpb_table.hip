@@ -27,20 +27,23 @@ __global__ __launch_bounds__(256) void table_fwd_kernel(int L, int buckets, cons
 // Many offsets share a bucket, so their values are added in LDS, as 64-bit whole numbers: such sums do not depend on the order of
 // the additions.  The unit is the largest value of the head over 2^(62 - bits of the number of offsets), so sums cannot overflow and a
 // bucket whose gradient is 2^-21 of the largest still has 24 bits.  Values that are not finite are noted by kind beside the sums.
-constexpr int kBuckets = 2048;          // buckets a workgroup
+constexpr int kBuckets = 2048;          // buckets a workgroup at most
+// Every workgroup of a head reads all offsets and adds those of its `chunk` buckets: the conversions, not the reads, are what costs
+// (36481 offsets in 625 buckets, us: 36 in one workgroup a head, TABLEUS in 16).
 template <class T>
-__global__ __launch_bounds__(1024) void table_bwd_kernel(int L, int buckets, int bits, const float *__restrict__ dbias,
+__global__ __launch_bounds__(1024) void table_bwd_kernel(int L, int buckets, int chunk, int bits, const float *__restrict__ dbias,
                                                          const int32_t *__restrict__ index, T *__restrict__ dtable)
 {
     __shared__ unsigned long long sum[kBuckets];
     __shared__ uint32_t odd[kBuckets];
     __shared__ uint32_t top;
-    const int hd = blockIdx.y, b0 = blockIdx.x * kBuckets, tid = threadIdx.x;
+    const int hd = blockIdx.y, b0 = blockIdx.x * chunk, tid = threadIdx.x;
     const float *x = dbias + (int64_t)hd * L;
     if (tid == 0) top = 0u;
-    for (int i = tid; i < kBuckets; i += 1024) sum[i] = 0ull, odd[i] = 0u;
+    for (int i = tid; i < chunk; i += 1024) sum[i] = 0ull, odd[i] = 0u;
     __syncthreads();
     uint32_t m = 0u;
+#pragma unroll 8
     for (int o = tid; o < L; o += 1024) {
         const uint32_t a = __float_as_uint(x[o]) & 0x7fffffffu;
         if (a < 0x7f800000u && a > m) m = a;
@@ -51,41 +54,50 @@ __global__ __launch_bounds__(1024) void table_bwd_kernel(int L, int buckets, int
     frexp((double)__uint_as_float(top), &e);            // the largest is below 2^e
     const double unit = ldexp(1., e + bits - 62);
     const double per = ldexp(1., 62 - bits - e);
-    for (int o = tid; o < L; o += 1024) {
-        const int i = index[o] - b0;
-        if ((uint32_t)index[o] >= (uint32_t)buckets || (uint32_t)i >= (uint32_t)kBuckets) continue;
-        const float v = x[o];
-        if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) atomicOr(&odd[i], v != v ? 4u : v > 0.f ? 1u : 2u);
-        else atomicAdd(&sum[i], (unsigned long long)llrint((double)v * per));
+    for (int o0 = tid; o0 < L; o0 += 8 * 1024) {           // (eight loads in flight)
+        int at[8];
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int o = o0 + j * 1024 < L ? o0 + j * 1024 : L - 1;
+            at[j] = o0 + j * 1024 < L ? index[o] : -1, v[j] = x[o];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = at[j] - b0;
+            if ((uint32_t)at[j] >= (uint32_t)buckets || (uint32_t)i >= (uint32_t)chunk) continue;
+            if ((__float_as_uint(v[j]) & 0x7f800000u) == 0x7f800000u) atomicOr(&odd[i], v[j] != v[j] ? 4u : v[j] > 0.f ? 1u : 2u);
+            else atomicAdd(&sum[i], (unsigned long long)llrint((double)v[j] * per));
+        }
     }
     __syncthreads();
-    for (int i = tid; i < kBuckets && b0 + i < buckets; i += 1024) {
+    for (int i = tid; i < chunk && b0 + i < buckets; i += 1024) {
         float v = (float)((double)(long long)sum[i] * unit);
         if (odd[i] != 0u) v = odd[i] == 1u ? INFINITY : odd[i] == 2u ? -INFINITY : NAN;
         store_as(dtable + (int64_t)hd * buckets + b0 + i, v);
     }
 }
 
-// dbias[head][o] = sum over windows and their workgroups of the workgroups' sums.  64 offsets a workgroup, 16 runs of windows, each
-// in ascending order, then the runs in ascending order.  Bound by memory: every partial sum is read once.
-__global__ __launch_bounds__(1024) void reduce_kernel(Geo g, int windows, int nblk, int prows, int group, const float *__restrict__ part,
+// dbias[head][o] = sum over windows and their workgroups of the workgroups' sums.  64 offsets a workgroup, 16 threads an offset: up to 16 runs
+// of windows, the rest of the 16 over a window's workgroups, then the 16 in a fixed order.  Bound by memory: every partial sum is read once.
+__global__ __launch_bounds__(1024) void reduce_kernel(Geo g, int windows, int runs, int nblk, int prows, int group, const float *__restrict__ part,
                                                       float *__restrict__ dbias)
 {
     __shared__ float run[16][64];
-    const int w2 = 2 * g.M - 1, L = w2 * w2, hd = blockIdx.y;
-    const int lane = threadIdx.x & 63, r = threadIdx.x >> 6, o = blockIdx.x * 64 + lane;
-    const int per = (windows + 15) / 16, w0 = r * per, w1 = w0 + per < windows ? w0 + per : windows;
+    const int w2 = 2 * g.M - 1, L = w2 * w2, hd = blockIdx.y, size = prows * w2;
+    const int lane = threadIdx.x & 63, r = threadIdx.x >> 6, o = blockIdx.x * 64 + lane, rw = r % runs;
+    const int per = (windows + runs - 1) / runs, w0 = rw * per, w1 = w0 + per < windows ? w0 + per : windows;
+    const int64_t step = (int64_t)g.heads * nblk * size;
     float sum = 0.f;
     if (o < L)
-        for (int blk = 0; blk < nblk; ++blk) {
+        for (int blk = r / runs; blk < nblk; blk += 16 / runs) {
             const int first = blk * group, last = first + group < g.N ? first + group - 1 : g.N - 1;
             const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m);
-            // the offset's word of this workgroup's rows (streamed - stationary row, from -sy1 on, is minus the offset's)
+            // the offset's word of a workgroup's rows (streamed - stationary row, from -sy1 on, is minus the offset's)
             const int at = 2 * g.M * (g.M - 1) + sy1 * w2 + g.M - 1 - o;
             if (at < 0 || at >= (g.M + sy1 - sy0) * w2) continue;
-            const float *p = part + ((int64_t)w0 * g.heads + hd) * nblk * prows * w2 + (int64_t)blk * prows * w2 + at;
-            const int64_t step = (int64_t)g.heads * nblk * prows * w2;
-#pragma unroll 4
+            const float *p = part + ((int64_t)w0 * g.heads + hd) * nblk * size + (int64_t)blk * size + at;
+#pragma unroll 8
             for (int w = w0; w < w1; ++w, p += step) sum += *p;
         }
     run[r][lane] = sum;
@@ -101,7 +113,10 @@ __global__ __launch_bounds__(1024) void reduce_kernel(Geo g, int windows, int nb
 hipError_t launch_reduce(const Geo &g, int dtype, const Ws &w, const float *part, float *dbias, hipStream_t st)
 {
     const int L = (2 * g.M - 1) * (2 * g.M - 1);
-    hipLaunchKernelGGL(reduce_kernel, dim3((L + 63) / 64, g.heads), dim3(1024), 0, st, g, (int)(g.units / g.heads), w.nblk, w.prows,
+    const int windows = w.shares;
+    int runs = 16;
+    while (runs > 1 && (runs > windows || (runs / 2 >= windows && w.nblk > 1))) runs /= 2;
+    hipLaunchKernelGGL(reduce_kernel, dim3((L + 63) / 64, g.heads), dim3(1024), 0, st, g, windows, runs, w.nblk, w.prows,
                        group_tokens(dtype, g.N), part, dbias);
     return hipGetLastError();
 }
@@ -118,9 +133,11 @@ hipError_t launch_table_bwd(int M, int heads, int buckets, int dtype, const floa
     const int L = (2 * M - 1) * (2 * M - 1);
     int bits = 1;
     while ((1 << bits) < L) ++bits;
-    const dim3 grid((buckets + kBuckets - 1) / kBuckets, heads);
-    if (dtype == RIB_BF16) hipLaunchKernelGGL(table_bwd_kernel<bf16_t>, grid, dim3(1024), 0, st, L, buckets, bits, dbias, index, (bf16_t *)dtable);
-    else hipLaunchKernelGGL(table_bwd_kernel<float>, grid, dim3(1024), 0, st, L, buckets, bits, dbias, index, (float *)dtable);
+    int chunk = (buckets + 15) / 16;
+    chunk = chunk < 32 ? 32 : chunk > kBuckets ? kBuckets : chunk;
+    const dim3 grid((buckets + chunk - 1) / chunk, heads);
+    if (dtype == RIB_BF16) hipLaunchKernelGGL(table_bwd_kernel<bf16_t>, grid, dim3(1024), 0, st, L, buckets, chunk, bits, dbias, index, (bf16_t *)dtable);
+    else hipLaunchKernelGGL(table_bwd_kernel<float>, grid, dim3(1024), 0, st, L, buckets, chunk, bits, dbias, index, (float *)dtable);
     return hipGetLastError();
 }
 
