@@ -102,40 +102,39 @@ __device__ __forceinline__ Raw scaled(Raw r, float s)
     return r;
 }
 
-// Token n of the window (clamped to the last one) as a pixel of its image.
-__device__ __forceinline__ uint32_t pixel(const Win &w, int n)
-{
-    const int iy = (int)__umulhi((uint32_t)n, w.inv_m);
-    return (uint32_t)(w.rowb[iy] + w.colo[n - __mul24(iy, w.M)]);
-}
+// A token as a pixel of its image.
+__device__ __forceinline__ uint32_t pixel(const Win &w, const Cell &c) { return (uint32_t)(w.rowb[c.y] + w.colo[c.x]); }
 
 // What a thread moves of a tile: LP lanes a token, P passes of nt lanes.
-template <int LP, int W, int SX, int SY, bool EXT>
+template <int LP, int W, int SX, int SY, bool EXT, bool ALN>
 struct Mover {
     static constexpr int NT = 64 * W, P = (kTile * LP + NT - 1) / NT;
     Raw x[P], y[P];
     uint2 e[EXT ? P : 1];
 
-    __device__ __forceinline__ void request(const Geo &g, const Win &win, const Rows &xs, const Rows &ys, const uint2 *ext, int tile)
+    __device__ __forceinline__ void request(const Geo &g, const Bias &bi, const Win &win, const Rows &xs, const Rows &ys, const uint2 *ext, int tile)
     {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const int slot = p * NT + threadIdx.x, row = slot / LP, j = slot % LP;
+            if (NT * P != kTile * LP && slot >= kTile * LP) break;
             const int n0 = tile * kTile + row, n = n0 < g.N ? n0 : g.N - 1;
-            const uint32_t t = SX == kCkpt && SY == kCkpt ? 0u : pixel(win, n);
-            x[p] = get_piece<SX>(xs, t, n, j, g.d);
-            y[p] = get_piece<SY>(ys, t, n, j, g.d);
+            const Cell c = cell_of<ALN>(g, bi, n);
+            const uint32_t t = SX == kCkpt && SY == kCkpt ? 0u : pixel(win, c);
+            x[p] = get_piece<SX>(xs, t, c.index(g), j, g.d);
+            y[p] = get_piece<SY>(ys, t, c.index(g), j, g.d);
             if (EXT) e[p] = ext[n];
         }
     }
     // KX, KY: the images' widths.  ONES: ones in the two last columns of both (dq); EXT: -LSE and -delta there (dkv).
-    template <int KX, int KY, bool ONES, bool ALN>
-    __device__ __forceinline__ void commit(const Geo &g, bf16_t *S, int tile, float scale)
+    template <int KX, int KY, bool ONES>
+    __device__ __forceinline__ void commit(const Geo &g, const Bias &bi, bf16_t *S, int tile, float scale)
     {
         using I = Img<KX, KY>;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const int slot = p * NT + threadIdx.x, row = slot / LP, j = slot % LP;
+            if (NT * P != kTile * LP && slot >= kTile * LP) break;
             const int n = tile * kTile + row;
             const bool in = ALN || n < g.N;
             bf16_t *xr = S + row * I::XS, *yr = S + I::YR + row * I::YS;
@@ -150,7 +149,7 @@ struct Mover {
                 *(uint32_t *)(xr + KX - 2) = in ? e[p].x : pack_bf16(-kNoRow, 0.f);
                 *(uint32_t *)(yr + KY - 2) = in ? e[p].y : 0u;
             }
-            if (!ALN && j == 0) ((int *)(S + I::LT))[row] = lin(g, in ? n : g.N - 1);
+            if (!ALN && j == 0) ((int *)(S + I::LT))[row] = cell_of<false>(g, bi, in ? n : g.N - 1).lin(bi);
         }
     }
 };
@@ -168,8 +167,8 @@ __device__ __forceinline__ void init_cols(const Geo &g, bf16_t *S, bool ones, bo
 
 // A wave's 64 stationary rows as B operands, through `area` (64 rows of K + 8 columns, the wave's own).
 // f(pass, lane-row, j, raw) may change a piece and gets to write columns of the row.
-template <int K, int LP, int SRC, class Fix>
-__device__ __forceinline__ void stationary_rows(const Geo &g, const Win &win, const Rows &s, int n0, bf16_t *area, bf16x8 (&B)[2][K / 16], Fix fix)
+template <int K, int LP, int SRC, bool ALN, class Fix>
+__device__ __forceinline__ void stationary_rows(const Geo &g, const Bias &bi, const Win &win, const Rows &s, int n0, bf16_t *area, bf16x8 (&B)[2][K / 16], Fix fix)
 {
     constexpr int STR = K + 8, R = 64 / LP;             // rows a pass
     const int lane = threadIdx.x & 63, l = lane / LP, j = lane % LP;
@@ -177,7 +176,8 @@ __device__ __forceinline__ void stationary_rows(const Geo &g, const Win &win, co
 #pragma unroll
     for (int p = 0; p < LP; ++p) {
         const int n = n0 + p * R + l, nc = n < g.N ? n : g.N - 1;
-        r[p] = get_piece<SRC>(s, SRC == kCkpt ? 0u : pixel(win, nc), nc, j, g.d);
+        const Cell c = cell_of<ALN>(g, bi, nc);
+        r[p] = get_piece<SRC>(s, SRC == kCkpt ? 0u : pixel(win, c), c.index(g), j, g.d);
     }
     {
         bf16_t *xr = area + lane * STR;
@@ -212,20 +212,21 @@ struct FixPair {
 // ---- blocks ------------------------------------------------------------------------------------------------------
 
 // LDS words of a lane's 16 streamed tokens of block `kb` of a tile, relative to the lane's own word (c0 - lin(stationary)).
-// Tokens 8a + 4 hf + 0..3: four neighbours each, unless M is no multiple of 8 (then from the tile's table).
+// Tokens 8a + 4 hf + 0..3: four neighbours each in strips (ALN), else from the tile's table.
 template <bool ALN>
 struct Words16 {
     int at[ALN ? 4 : 16];
     __device__ __forceinline__ int operator()(int i) const { return ALN ? at[i >> 2] + (i & 3) : at[ALN ? 0 : i]; }
 };
 template <bool ALN>
-__device__ __forceinline__ Words16<ALN> words_of(const Geo &g, const int *table, int tile, int kb, int hf)
+__device__ __forceinline__ Words16<ALN> words_of(const Bias &bi, const Chunk &ch, const int *table, int tile, int kb, int hf)
 {
     Words16<ALN> w;
 #pragma unroll
     for (int a = 0; a < 4; ++a) {
         if constexpr (ALN) {
-            w.at[a] = lin(g, tile * kTile + kb * 32 + 8 * a) + 4 * hf;      // (all but 4 hf uniform)
+            const int r = tile * kTile + kb * 32 + 8 * a - ch.t0;       // (all but 4 hf uniform)
+            w.at[a] = (r >> bi.sh) * bi.ws + (r & (bi.sw - 1)) + 4 * hf;
         } else {
             const int4 t = *(const int4 *)(table + kb * 32 + 8 * a + 4 * hf);
             w.at[4 * a] = t.x, w.at[4 * a + 1] = t.y, w.at[4 * a + 2] = t.z, w.at[4 * a + 3] = t.w;
@@ -310,15 +311,15 @@ constexpr size_t stage_bytes()
 // ---- forward -----------------------------------------------------------------------------------------------------
 
 // One walk over the keys.  MAX: with the running maximum of every row.
-template <bool MAX, int KX, int DB, bool SUM, int SRC, bool ALN, bool CARRY, int W>
+template <bool MAX, int KX, int DB, bool SUM, int SRC, bool ALN, int W>
 __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Place &pl, const Rows &ks, const Rows &vs, bf16_t *S, float *B,
-                                         const bf16x8 (&Q)[2][KX / 16], f32x16 (&O)[2][DB], float (&sum)[2], float (&top)[2], int sy0, int sy1,
+                                         const bf16x8 (&Q)[2][KX / 16], f32x16 (&O)[2][DB], float (&sum)[2], float (&top)[2], const Span &span,
                                          const int (&mylin)[2], bool active)
 {
     constexpr int LP = KX <= 32 ? 4 : 8, KY = 32 * DB, NT = 64 * W;
     using I = Img<KX, KY>;
     const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5;
-    const int ntiles = (g.N + kTile - 1) / kTile;
+    const int ntiles = (g.N + kTile - 1) / kTile, strip_tiles = ALN ? bi.strip / kTile : ntiles;
     const int tro = tr_lane_offset<I::YS>(lane), ako = col * I::XS + 8 * hf;
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
@@ -328,29 +329,29 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
             for (int i = 0; i < 16; ++i) O[qb][db][i] = 0.f;
         sum[qb] = 0.f, top[qb] = MAX ? -INFINITY : 0.f;
     }
-    Mover<LP, W, SRC, SRC, false> mv;
-    mv.request(g, pl.win, ks, vs, nullptr, 0);
-    mv.template commit<KX, KY, false, ALN>(g, S, 0, 1.f);
-    mv.request(g, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
-    f32x16 next;            // (CARRY) the bias of block (1, the coming one)
-    for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
-        const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
-        const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
+    Mover<LP, W, SRC, SRC, false, ALN> mv;
+    mv.request(g, bi, pl.win, ks, vs, nullptr, 0);
+    mv.template commit<KX, KY, false>(g, bi, S, 0, 1.f);
+    mv.request(g, bi, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
+    f32x16 next;            // (ALN) the bias of block (1, the coming one)
+    for (int t0 = 0, t1, end = strip_tiles; t0 < ntiles; t0 = t1) {
+        t1 = t0 + bi.chunk < end ? t0 + bi.chunk : end;
+        const Chunk ch = chunk_of<ALN>(g, bi, t0, t1, span);
         stage_bias<-1>(g, bi, ch, pl.hd, bi.bs, B, NT);
         __syncthreads();
-        if (CARRY && t0 == 0 && active) next = bias_block<ALN>(B + ch.c0 - mylin[1], words_of<ALN>(g, nullptr, 0, 0, hf));
+        if (ALN && t0 * kTile == ch.t0 && active) next = bias_block<ALN>(B + ch.c0 - mylin[1], words_of<ALN>(bi, ch, nullptr, t0, 0, hf));
         for (int tile = t0; tile < t1; ++tile) {
             const bf16_t *cur = S + (tile & 1) * I::STAGE;
             if (tile + 1 < ntiles) {
-                mv.template commit<KX, KY, false, ALN>(g, S + ((tile + 1) & 1) * I::STAGE, tile + 1, 1.f);
-                mv.request(g, pl.win, ks, vs, nullptr, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
+                mv.template commit<KX, KY, false>(g, bi, S + ((tile + 1) & 1) * I::STAGE, tile + 1, 1.f);
+                mv.request(g, bi, pl.win, ks, vs, nullptr, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
             }
             if (active) {
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb) {
                     const int key0 = tile * kTile + kb * 32;
                     if (!ALN && key0 >= g.N) break;
-                    const Words16<ALN> wd = words_of<ALN>(g, (const int *)(cur + I::LT), tile, kb, hf);
+                    const Words16<ALN> wd = words_of<ALN>(bi, ch, (const int *)(cur + I::LT), tile, kb, hf);
                     bf16x8 Ak[KX / 16], At[DB][2];
                     read_rows<KX / 16>(Ak, cur + kb * 32 * I::XS + ako);
 #pragma unroll
@@ -360,8 +361,8 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
 #pragma unroll
                     for (int qx = 0; qx < 2; ++qx) {
                         const int qb = 1 - qx;
-                        f32x16 s = CARRY && qb == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[qb], wd);
-                        if (CARRY && qb == 0) next = s;
+                        f32x16 s = ALN && qb == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[qb], wd);
+                        if (ALN && qb == 0) next = s;
 #pragma unroll
                         for (int i = 0; i < KX / 16; ++i) s = mfma(Ak[i], Q[qb][i], s);
                         if (!ALN) mask_rows(s, key0, g.N, hf);
@@ -404,6 +405,7 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
             }
             __syncthreads();
         }
+        if (t1 == end) end += strip_tiles;
     }
     // the denominator: the last row of O^T is register 15 of the upper lane half
 #pragma unroll
@@ -413,8 +415,8 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
     }
 }
 
-template <int KX, int DB, bool SUM, int SRC, bool ALN, bool CARRY, int W>
-__global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void fwd_kernel(Geo g, Bias bi, int nblk, int force_max, const bf16_t *__restrict__ q,
+template <int KX, int DB, bool SUM, int SRC, bool ALN, int W>
+__global__ __launch_bounds__(W * 64, 2) void fwd_kernel(Geo g, Bias bi, int nblk, int force_max, const bf16_t *__restrict__ q,
                                                         const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
                                                         bf16_t *__restrict__ out, float *__restrict__ lse)
 {
@@ -427,15 +429,15 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void fwd_kernel(Geo g, Bias
     const Place pl = place_of(g, nblk, NT, map);
     __syncthreads();
     const int first = pl.blk * NT, last = first + NT < g.N ? first + NT - 1 : g.N - 1, n0 = first + wave * 64;
-    const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m);
+    const Span span = span_of<ALN>(g, bi, first, last);
     const bool active = n0 < g.N;
     bf16x8 Q[2][KX / 16];
-    stationary_rows<KX, LP, SRC>(g, pl.win, grid_rows(g, pl, q, g.tstride), n0, S + wave * 64 * (KX + 8), Q, FixScale{bi.qs});
+    stationary_rows<KX, LP, SRC, ALN>(g, bi, pl.win, grid_rows(g, pl, q, g.tstride), n0, S + wave * 64 * (KX + 8), Q, FixScale{bi.qs});
     int mylin[2];
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
         const int n = n0 + qb * 32 + col;
-        mylin[qb] = lin(g, n < g.N ? n : g.N - 1);
+        mylin[qb] = cell_of<ALN>(g, bi, n < g.N ? n : g.N - 1).lin(bi);
     }
     __syncthreads();
     init_cols<KX, 32 * DB>(g, S, false, !SUM, NT);
@@ -447,21 +449,22 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void fwd_kernel(Geo g, Bias
     // denominator leaves [2^-60, 2^60], and not for want of keys, sends the workgroup on a second walk, with one.
     bool bad = true;
     if (!force_max) {
-        fwd_walk<false, KX, DB, SUM, SRC, ALN, CARRY, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, sy0, sy1, mylin, active);
+        fwd_walk<false, KX, DB, SUM, SRC, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, mylin, active);
         bad = false;
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb)
-            if (active && bad_rows(g, bi, pl.hd, n0 + qb * 32 + col, sum[qb])) bad = true;
+            if (active && bad_rows(g, bi, pl.hd, n0 + qb * 32 + col < g.N ? cell_of<ALN>(g, bi, n0 + qb * 32 + col).index(g) : g.N, sum[qb])) bad = true;
     }
-    if (__syncthreads_or(bad)) fwd_walk<true, KX, DB, SUM, SRC, ALN, CARRY, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, sy0, sy1, mylin, active);
+    if (__syncthreads_or(bad)) fwd_walk<true, KX, DB, SUM, SRC, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, mylin, active);
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
         const int n = n0 + qb * 32 + col;
         if (n >= g.N) continue;
+        const Cell c = cell_of<ALN>(g, bi, n);
         const float inv = sum[qb] == 0.f ? 0.f : 1.f / sum[qb];         // (a row without a key: zeros)
         if (lse != nullptr && hf == 0)
-            lse[(int64_t)pl.u * g.N + n] = sum[qb] == 0.f ? -INFINITY : (top[qb] + __builtin_amdgcn_logf(sum[qb])) * kLn2;
-        bf16_t *row = out + (pl.img + pixel(pl.win, n)) * g.C + pl.hd * g.d;
+            lse[(int64_t)pl.u * g.N + c.index(g)] = sum[qb] == 0.f ? -INFINITY : (top[qb] + __builtin_amdgcn_logf(sum[qb])) * kLn2;
+        bf16_t *row = out + (pl.img + pixel(pl.win, c)) * g.C + pl.hd * g.d;
 #pragma unroll
         for (int db = 0; db < DB; ++db) store_row<SRC>(row, O[qb][db], db, g.d, hf, inv);
     }
@@ -469,8 +472,8 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void fwd_kernel(Geo g, Bias
 
 // ---- backward: dq and the bias's gradient -------------------------------------------------------------------------
 
-template <int K, int DB, int SRC, int SG, bool ALN, bool CARRY, int W, bool HIST>
-__global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias bi, int nblk, int prows, const bf16_t *__restrict__ q,
+template <int K, int DB, int SRC, int SG, bool ALN, int W, bool HIST>
+__global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk, const bf16_t *__restrict__ q,
                                                        const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
                                                        const uint8_t *__restrict__ ckpt, const bf16_t *__restrict__ out,
                                                        const bf16_t *__restrict__ dout, const float *__restrict__ lse,
@@ -482,15 +485,15 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
     bf16_t *S = (bf16_t *)smem;
     int *map = (int *)(smem + stage_bytes<K, K, W>());
     float *B = (float *)(map + 2 * g.M);
-    double *H = (double *)(B + ((bi.rows * bi.w2 + 1) & ~1));           // [wave][hrows * w2]
-    const int hsize = bi.hrows * bi.w2;
+    double *H = (double *)(B + ((bi.rows * bi.ws + 1) & ~1));           // [wave][hrows * w2]
+    const int hsize = bi.hrows * bi.ws;
     const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place pl = place_of(g, nblk, NT, map);
     if (HIST)
         for (int e = threadIdx.x; e < W * hsize; e += NT) H[e] = 0.;
     __syncthreads();
     const int first = pl.blk * NT, last = first + NT < g.N ? first + NT - 1 : g.N - 1, n0 = first + wave * 64;
-    const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m);
+    const Span span = span_of<ALN>(g, bi, first, last);
     const bool active = n0 < g.N;
     bf16x8 Q[2][K / 16], D[2][K / 16];
     float L;            // LSE in base 2 of row `lane`
@@ -502,8 +505,8 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
 #pragma unroll
         for (int p = 0; p < LP; ++p) {
             const int n = n0 + p * (64 / LP) + l, nc = n < g.N ? n : g.N - 1;
-            const uint32_t t = pixel(pl.win, nc);
-            const Raw a = get_piece<SG>(os, t, nc, j, g.d), b = get_piece<SG>(ds, t, nc, j, g.d);
+            const uint32_t t = pixel(pl.win, cell_of<ALN>(g, bi, nc));
+            const Raw a = get_piece<SG>(os, t, 0, j, g.d), b = get_piece<SG>(ds, t, 0, j, g.d);
             float s = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {       // (a piece that slid back holds a neighbour's values first)
@@ -522,26 +525,26 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
             if (lane / (64 / LP) == p) delta = x;
         }
         const int n = n0 + lane, nc = n < g.N ? n : g.N - 1;
-        const float e = lse[(int64_t)pl.u * g.N + nc];
+        const float e = lse[(int64_t)pl.u * g.N + cell_of<ALN>(g, bi, nc).index(g)];
         const bool none = n >= g.N || e == -INFINITY;
         const uint32_t wl = none ? pack_bf16(-kNoRow, 0.f) : split_bf16(-e * bi.bs), wd = split_bf16(-delta);
         L = none ? kNoRow : e * kLog2e;
         if (n < g.N) ext[(int64_t)pl.u * g.N + n] = uint2{wl, wd};
         bf16_t *area = S + wave * 64 * (K + 8);
         const Rows qs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 0) : grid_rows(g, pl, q, g.tstride);
-        stationary_rows<K, LP, SRC>(g, pl.win, qs, n0, area, Q, FixScale{bi.qs});
-        stationary_rows<K, LP, SG>(g, pl.win, ds, n0, area, D, FixPair<K>{wd});
+        stationary_rows<K, LP, SRC, ALN>(g, bi, pl.win, qs, n0, area, Q, FixScale{bi.qs});
+        stationary_rows<K, LP, SG, ALN>(g, bi, pl.win, ds, n0, area, D, FixPair<K>{wd});
     }
     int mylin[2];
     float mylse[2];
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
         const int n = n0 + qb * 32 + col;
-        mylin[qb] = lin(g, n < g.N ? n : g.N - 1);
+        mylin[qb] = cell_of<ALN>(g, bi, n < g.N ? n : g.N - 1).lin(bi);
         mylse[qb] = __shfl(L, qb * 32 + col);
     }
     // (the wave's own last window row, for its histogram)
-    const int wsy1 = row_of(n0 + 63 < g.N ? n0 + 63 : g.N - 1, g.inv_m);
+    const int wsy1 = span_of<ALN>(g, bi, n0 < g.N ? n0 : g.N - 1, n0 + 63 < g.N ? n0 + 63 : g.N - 1).y1;
     __syncthreads();
     init_cols<K, K>(g, S, true, false, NT);
     __syncthreads();
@@ -554,35 +557,35 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
         for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int i = 0; i < 16; ++i) A[qb][db][i] = 0.f;
-    const int ntiles = (g.N + kTile - 1) / kTile;
+    const int ntiles = (g.N + kTile - 1) / kTile, strip_tiles = ALN ? bi.strip / kTile : ntiles;
     const int tro = tr_lane_offset<I::XS>(lane), ako = col * I::XS + 8 * hf;
     const f32x16 z = {0};
-    Mover<LP, W, SRC, SRC, false> mv;
-    mv.request(g, pl.win, ks, vs, nullptr, 0);
-    mv.template commit<K, K, true, ALN>(g, S, 0, 1.f);
-    mv.request(g, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
-    f32x16 next, held;      // (CARRY) the bias of block (1, the coming one); dS of block (0, the last one)
-    if (CARRY && HIST) held = z;
-    int before = -1;            // last streamed row of the chunk before
-    for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
-        const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
-        const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
+    Mover<LP, W, SRC, SRC, false, ALN> mv;
+    mv.request(g, bi, pl.win, ks, vs, nullptr, 0);
+    mv.template commit<K, K, true>(g, bi, S, 0, 1.f);
+    mv.request(g, bi, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
+    f32x16 next, held;      // (ALN) the bias of block (1, the coming one); dS of block (0, the last one)
+    if (ALN && HIST) held = z;
+    int before = -1;            // last streamed row of the strip's chunk before
+    for (int t0 = 0, t1, end = strip_tiles; t0 < ntiles; t0 = t1) {
+        t1 = t0 + bi.chunk < end ? t0 + bi.chunk : end;
+        const Chunk ch = chunk_of<ALN>(g, bi, t0, t1, span);
         stage_bias<-1>(g, bi, ch, pl.hd, bi.bs, B, NT);
-        double *const mine = H + wave * hsize + ch.c0 - (sy1 - wsy1) * bi.w2;
+        double *const mine = H + wave * hsize + ch.c0 - (span.y1 - wsy1) * bi.ws;
         __syncthreads();
-        if (CARRY && t0 == 0 && active) next = bias_block<ALN>(B + ch.c0 - mylin[1], words_of<ALN>(g, nullptr, 0, 0, hf));
+        if (ALN && t0 * kTile == ch.t0 && active) next = bias_block<ALN>(B + ch.c0 - mylin[1], words_of<ALN>(bi, ch, nullptr, t0, 0, hf));
         for (int tile = t0; tile < t1; ++tile) {
             const bf16_t *cur = S + (tile & 1) * I::STAGE;
             if (tile + 1 < ntiles) {
-                mv.template commit<K, K, true, ALN>(g, S + ((tile + 1) & 1) * I::STAGE, tile + 1, 1.f);
-                mv.request(g, pl.win, ks, vs, nullptr, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
+                mv.template commit<K, K, true>(g, bi, S + ((tile + 1) & 1) * I::STAGE, tile + 1, 1.f);
+                mv.request(g, bi, pl.win, ks, vs, nullptr, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
             }
             if (active) {
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb) {
                     const int key0 = tile * kTile + kb * 32;
                     if (!ALN && key0 >= g.N) break;
-                    const Words16<ALN> wd = words_of<ALN>(g, (const int *)(cur + I::LT), tile, kb, hf);
+                    const Words16<ALN> wd = words_of<ALN>(bi, ch, (const int *)(cur + I::LT), tile, kb, hf);
                     bf16x8 Ak[K / 16], Av[K / 16], At[DB][2];
                     read_rows<K / 16>(Ak, cur + kb * 32 * I::XS + ako);
                     read_rows<K / 16>(Av, cur + I::YR + kb * 32 * I::YS + ako);
@@ -593,8 +596,8 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
 #pragma unroll
                     for (int qx = 0; qx < 2; ++qx) {
                         const int qb = 1 - qx;
-                        f32x16 s = CARRY && qb == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[qb], wd), p = z;
-                        if (CARRY && qb == 0) next = s;
+                        f32x16 s = ALN && qb == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[qb], wd), p = z;
+                        if (ALN && qb == 0) next = s;
 #pragma unroll
                         for (int i = 0; i < K / 16; ++i) s = mfma(Ak[i], Q[qb][i], s);
 #pragma unroll
@@ -602,8 +605,8 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
                         if (!ALN) mask_rows(s, key0, g.N, hf);
 #pragma unroll
                         for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], bi.c, -mylse[qb])) * p[i];
-                        if (HIST && CARRY && qb == 1) add_offsets<ALN>(mine - mylin[1], wd, s + held);
-                        else if (HIST && CARRY) held = s;
+                        if (HIST && ALN && qb == 1) add_offsets<ALN>(mine - mylin[1], wd, s + held);
+                        else if (HIST && ALN) held = s;
                         else if (HIST && (ALN || n0 + qb * 32 + col < g.N)) add_offsets<ALN>(mine - mylin[qb], wd, s);     // (many lanes at one word are slow)
                         uint32_t P[8];
 #pragma unroll
@@ -619,20 +622,22 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
             __syncthreads();
         }
         if (HIST) {
-            if (CARRY && t1 == ntiles) {
-                if (active) add_offsets<ALN>(mine - mylin[0], words_of<ALN>(g, nullptr, ntiles - 1, 1, hf), held);
+            if (ALN && t1 == end) {
+                if (active) add_offsets<ALN>(mine - mylin[0], words_of<ALN>(bi, ch, nullptr, t1 - 1, 1, hf), held);
+                held = z;
                 __syncthreads();
             }
-            flush<W, 64>(g, bi, ch, H, hsize, first, sy0, sy1, before,
-                         part + ((int64_t)pl.u * nblk + pl.blk) * prows * bi.w2 + ch.ty0 * bi.w2);
-            before = ch.ty1;
+            flush<ALN, W, 64>(g, bi, ch, H, hsize, first, before,
+                              part + sums_at(g, bi, pl.u, nblk, pl.blk, bi.prows, ch.t.x0) + ch.t.y0 * bi.ws);
+            before = t1 == end ? -1 : ch.t.y1;
         }
+        if (t1 == end) end += strip_tiles;
     }
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
         const int n = n0 + qb * 32 + col;
         if (n >= g.N) continue;
-        bf16_t *row = dq + (pl.img + pixel(pl.win, n)) * g.C + pl.hd * g.d;
+        bf16_t *row = dq + (pl.img + pixel(pl.win, cell_of<ALN>(g, bi, n))) * g.C + pl.hd * g.d;
 #pragma unroll
         for (int db = 0; db < DB; ++db) store_row<SG>(row, A[qb][db], db, g.d, hf, g.scale_c);
     }
@@ -640,8 +645,8 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
 
 // ---- backward: dk, dv --------------------------------------------------------------------------------------------
 
-template <int K, int DB, int SRC, int SG, bool ALN, bool CARRY, int W>
-__global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias bi, int nblk, const bf16_t *__restrict__ q,
+template <int K, int DB, int SRC, int SG, bool ALN, int W>
+__global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk, const bf16_t *__restrict__ q,
                                                         const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
                                                         const uint8_t *__restrict__ ckpt, const bf16_t *__restrict__ dout,
                                                         const uint2 *__restrict__ ext, bf16_t *__restrict__ dk, bf16_t *__restrict__ dv)
@@ -656,21 +661,21 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
     const Place pl = place_of(g, nblk, NT, map);
     __syncthreads();
     const int first = pl.blk * NT, last = first + NT < g.N ? first + NT - 1 : g.N - 1, n0 = first + wave * 64;
-    const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m);
+    const Span span = span_of<ALN>(g, bi, first, last);
     const bool active = n0 < g.N;
     bf16x8 Kb[2][K / 16], Vb[2][K / 16];
     {
         bf16_t *area = S + wave * 64 * (K + 8);
         const Rows ks = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 1) : grid_rows(g, pl, k, g.tstride);
         const Rows vs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 2) : grid_rows(g, pl, v, g.tstride);
-        stationary_rows<K, LP, SRC>(g, pl.win, ks, n0, area, Kb, FixPair<K>{kOnes});
-        stationary_rows<K, LP, SRC>(g, pl.win, vs, n0, area, Vb, FixPair<K>{kOnes});
+        stationary_rows<K, LP, SRC, ALN>(g, bi, pl.win, ks, n0, area, Kb, FixPair<K>{kOnes});
+        stationary_rows<K, LP, SRC, ALN>(g, bi, pl.win, vs, n0, area, Vb, FixPair<K>{kOnes});
     }
     int mylin[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
         const int n = n0 + b * 32 + col;
-        mylin[b] = lin(g, n < g.N ? n : g.N - 1);
+        mylin[b] = cell_of<ALN>(g, bi, n < g.N ? n : g.N - 1).lin(bi);
     }
     __syncthreads();
     init_cols<K, K>(g, S, false, false, NT);
@@ -684,32 +689,32 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
         for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int i = 0; i < 16; ++i) Ak[b][db][i] = 0.f, Av[b][db][i] = 0.f;
-    const int ntiles = (g.N + kTile - 1) / kTile;
+    const int ntiles = (g.N + kTile - 1) / kTile, strip_tiles = ALN ? bi.strip / kTile : ntiles;
     const int tro = tr_lane_offset<I::XS>(lane), ako = col * I::XS + 8 * hf;
     const float scale = bi.qs;
     const f32x16 z = {0};
-    f32x16 next;            // (CARRY) the bias of block (1, the coming one)
-    Mover<LP, W, SRC, SG, true> mv;
-    mv.request(g, pl.win, qs, ds, ex, 0);
-    mv.template commit<K, K, false, ALN>(g, S, 0, scale);
-    mv.request(g, pl.win, qs, ds, ex, ntiles > 1 ? 1 : 0);
-    for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
-        const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
-        const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
+    f32x16 next;            // (ALN) the bias of block (1, the coming one)
+    Mover<LP, W, SRC, SG, true, ALN> mv;
+    mv.request(g, bi, pl.win, qs, ds, ex, 0);
+    mv.template commit<K, K, false>(g, bi, S, 0, scale);
+    mv.request(g, bi, pl.win, qs, ds, ex, ntiles > 1 ? 1 : 0);
+    for (int t0 = 0, t1, end = strip_tiles; t0 < ntiles; t0 = t1) {
+        t1 = t0 + bi.chunk < end ? t0 + bi.chunk : end;
+        const Chunk ch = chunk_of<ALN>(g, bi, t0, t1, span);
         stage_bias<1>(g, bi, ch, pl.hd, bi.bs, B, NT);
         __syncthreads();
-        if (CARRY && t0 == 0 && active) next = bias_block<ALN>(B + ch.c0 - mylin[1], words_of<ALN>(g, nullptr, 0, 0, hf));
+        if (ALN && t0 * kTile == ch.t0 && active) next = bias_block<ALN>(B + ch.c0 - mylin[1], words_of<ALN>(bi, ch, nullptr, t0, 0, hf));
         for (int tile = t0; tile < t1; ++tile) {
             const bf16_t *cur = S + (tile & 1) * I::STAGE;
             if (tile + 1 < ntiles) {
-                mv.template commit<K, K, false, ALN>(g, S + ((tile + 1) & 1) * I::STAGE, tile + 1, scale);
-                mv.request(g, pl.win, qs, ds, ex, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
+                mv.template commit<K, K, false>(g, bi, S + ((tile + 1) & 1) * I::STAGE, tile + 1, scale);
+                mv.request(g, bi, pl.win, qs, ds, ex, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
             }
             if (active) {
 #pragma unroll
                 for (int qb = 0; qb < 2; ++qb) {
                     if (!ALN && tile * kTile + qb * 32 >= g.N) break;
-                    const Words16<ALN> wd = words_of<ALN>(g, (const int *)(cur + I::LT), tile, qb, hf);
+                    const Words16<ALN> wd = words_of<ALN>(bi, ch, (const int *)(cur + I::LT), tile, qb, hf);
                     bf16x8 Aq[K / 16], Ad[K / 16], Tq[DB][2], Td[DB][2];
                     read_rows<K / 16>(Aq, cur + qb * 32 * I::XS + ako);
                     read_rows<K / 16>(Ad, cur + I::YR + qb * 32 * I::YS + ako);
@@ -723,8 +728,8 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
 #pragma unroll
                     for (int bx = 0; bx < 2; ++bx) {
                         const int b = 1 - bx;
-                        f32x16 s = CARRY && b == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[b], wd), p = z;
-                        if (CARRY && b == 0) next = s;
+                        f32x16 s = ALN && b == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[b], wd), p = z;
+                        if (ALN && b == 0) next = s;
 #pragma unroll
                         for (int i = 0; i < K / 16; ++i) s = mfma(Aq[i], Kb[b][i], s);
 #pragma unroll
@@ -749,12 +754,13 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
             }
             __syncthreads();
         }
+        if (t1 == end) end += strip_tiles;
     }
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
         const int n = n0 + b * 32 + col;
         if (n >= g.N) continue;
-        const int64_t at = (pl.img + pixel(pl.win, n)) * g.C + pl.hd * g.d;
+        const int64_t at = (pl.img + pixel(pl.win, cell_of<ALN>(g, bi, n))) * g.C + pl.hd * g.d;
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
             store_row<SG>(dk + at, Ak[b][db], db, g.d, hf, bi.ks);
@@ -767,53 +773,50 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
 
 constexpr size_t kBiasBytes = 36 * 1024, kHistBytes = 9 * 1024;
 
-// Whether the offsets of block (b + 1, t + 1), of stationary and streamed blocks of 32, are those of (b, t), lane by lane: 32 tokens on is whole
-// window rows on for both.  A wave then carries what belongs to a block's offsets over to the next step.
-inline bool carries(const Geo &g) { return g.M == 32 || g.M == 16; }
-
-template <int KX, int DB, bool SUM, int SRC, bool ALN, bool CARRY, int W>
+template <int KX, int DB, bool SUM, int SRC, bool ALN, int W>
 hipError_t launch_fwd_one(const Geo &g, const FwdArgs &a)
 {
     Bias bi{a.bias};
     plan_scale(g, &bi);
-    plan_chunks(g, RIB_BF16, &bi, false, kBiasBytes, 0);
+    plan_chunks(g, RIB_BF16, &bi, ALN, false, kBiasBytes, 0);
     const int nblk = (g.N + 64 * W - 1) / (64 * W);
-    const size_t smem = stage_bytes<KX, 32 * DB, W>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.w2 * 4;
+    const size_t smem = stage_bytes<KX, 32 * DB, W>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.ws * 4;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
-    auto kern = fwd_kernel<KX, DB, SUM, SRC, ALN, CARRY, W>;
+    auto kern = fwd_kernel<KX, DB, SUM, SRC, ALN, W>;
     const hipError_t e = prepare_kernel((const void *)kern, nullptr);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * nblk)), dim3(64 * W), smem, a.st, g, bi, nblk, a.force_max, (const bf16_t *)a.q,
                        (const bf16_t *)a.k, (const bf16_t *)a.v, (bf16_t *)a.out, a.lse);
     return hipGetLastError();
 }
-template <int K, int DB, int SRC, int SG, bool ALN, bool CARRY, int W, bool HIST>
+template <int K, int DB, int SRC, int SG, bool ALN, int W, bool HIST>
 hipError_t launch_dq_one(const Geo &g, const BwdArgs &a, const Ws &ws)
 {
     Bias bi{a.bias};
     plan_scale(g, &bi);
-    plan_chunks(g, RIB_BF16, &bi, HIST, kBiasBytes, kHistBytes);
-    const size_t smem = stage_bytes<K, K, W>() + 8 * (size_t)g.M + ((size_t)bi.rows * bi.w2 + 1) / 2 * 8 + (size_t)W * bi.hrows * bi.w2 * 8;
+    plan_chunks(g, RIB_BF16, &bi, ALN, HIST, kBiasBytes, kHistBytes);
+    const size_t smem = stage_bytes<K, K, W>() + 8 * (size_t)g.M + ((size_t)bi.rows * bi.ws + 1) / 2 * 8 + (size_t)W * bi.hrows * bi.ws * 8;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
-    auto kern = dq_kernel<K, DB, SRC, SG, ALN, CARRY, W, HIST>;
+    auto kern = dq_kernel<K, DB, SRC, SG, ALN, W, HIST>;
     const hipError_t e = prepare_kernel((const void *)kern, nullptr);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * ws.nblk)), dim3(64 * W), smem, a.st, g, bi, ws.nblk, ws.prows, (const bf16_t *)a.q,
+    hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * ws.nblk)), dim3(64 * W), smem, a.st, g, bi, ws.nblk, (const bf16_t *)a.q,
                        (const bf16_t *)a.k, (const bf16_t *)a.v, a.ckpt, (const bf16_t *)a.out, (const bf16_t *)a.dout, a.lse,
                        (bf16_t *)a.dq, (uint2 *)((char *)a.ws + ws.ext), (float *)((char *)a.ws + ws.part));
     return hipGetLastError();
 }
-template <int K, int DB, int SRC, int SG, bool ALN, bool CARRY, int W>
-hipError_t launch_pair(const Geo &g, const BwdArgs &a, const Ws &ws)
+template <int K, int DB, int SRC, int SG, bool ALN, int W>
+hipError_t launch_pair(const Geo &g, const BwdArgs &a, Ws &ws)
 {
-    hipError_t e = a.dbias != nullptr ? launch_dq_one<K, DB, SRC, SG, ALN, CARRY, W, true>(g, a, ws) : launch_dq_one<K, DB, SRC, SG, ALN, CARRY, W, false>(g, a, ws);
+    ws.strips = ALN;
+    hipError_t e = a.dbias != nullptr ? launch_dq_one<K, DB, SRC, SG, ALN, W, true>(g, a, ws) : launch_dq_one<K, DB, SRC, SG, ALN, W, false>(g, a, ws);
     if (e != hipSuccess) return e;
     Bias bi{a.bias};
     plan_scale(g, &bi);
-    plan_chunks(g, RIB_BF16, &bi, false, kBiasBytes, 0);
-    const size_t smem = stage_bytes<K, K, W>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.w2 * 4;
+    plan_chunks(g, RIB_BF16, &bi, ALN, false, kBiasBytes, 0);
+    const size_t smem = stage_bytes<K, K, W>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.ws * 4;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
-    auto kern = dkv_kernel<K, DB, SRC, SG, ALN, CARRY, W>;
+    auto kern = dkv_kernel<K, DB, SRC, SG, ALN, W>;
     e = prepare_kernel((const void *)kern, nullptr);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * ws.nblk)), dim3(64 * W), smem, a.st, g, bi, ws.nblk, (const bf16_t *)a.q,

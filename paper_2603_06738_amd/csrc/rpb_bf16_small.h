@@ -106,7 +106,7 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
     float *B = (float *)(smem + I::STAGE * 2 + 64);
     const int lane = threadIdx.x, col = lane & 31, hf = lane >> 5, nb = (g.N + 31) / 32;
     const Share sh = share_of(g, windows, per);
-    const Chunk ch = chunk_of(g, bi, 0, 1, 0, g.M - 1);
+    const Chunk ch = chunk_of<false>(g, bi, 0, 1, Span{0, g.M - 1, 0});
     stage_bias<-1>(g, bi, ch, sh.hd, bi.bs, B, 64);
     clear_image<KX>(g, X, 0u);
     clear_image<KY>(g, Y, 0u);
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
                     if (kb >= nb) break;
                     bf16x8 A[KX / 16];
                     read_rows<KX / 16>(A, X + kb * 32 * I::XS + ako);
-                    s[kb] = bias_block<false>(B + ch.c0 - mylin[qb], words_of<false>(g, table, 0, kb, hf));
+                    s[kb] = bias_block<false>(B + ch.c0 - mylin[qb], words_of<false>(bi, ch, table, 0, kb, hf));
 #pragma unroll
                     for (int i = 0; i < KX / 16; ++i) s[kb] = mfma(A[i], Q[qb][i], s[kb]);
                     if (kb == nb - 1) mask_rows(s[kb], kb * 32, g.N, hf);
@@ -239,7 +239,7 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
     const int lane = threadIdx.x, col = lane & 31, hf = lane >> 5, nb = (g.N + 31) / 32;
     const int l = lane / LP, j = lane % LP;
     const Share sh = share_of(g, windows, per);
-    const Chunk ch = chunk_of(g, bi, 0, 1, 0, g.M - 1);
+    const Chunk ch = chunk_of<false>(g, bi, 0, 1, Span{0, g.M - 1, 0});
     stage_bias<-1>(g, bi, ch, sh.hd, bi.bs, B, 64);
     if (HIST)
         for (int e = lane; e < count; e += 64) H[e] = 0.;
@@ -333,7 +333,7 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
 #pragma unroll
             for (int db = 0; db < DB; ++db) A[db] = z;
             for (int kb = 0; kb < nb; ++kb) {
-                const Words16<false> at = words_of<false>(g, table, 0, kb, hf);
+                const Words16<false> at = words_of<false>(bi, ch, table, 0, kb, hf);
                 bf16x8 Ak[K / 16], Av[K / 16];
                 read_rows<K / 16>(Ak, X + kb * 32 * XS + ako);
                 read_rows<K / 16>(Av, Y + kb * 32 * XS + ako);
@@ -377,7 +377,7 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
 #pragma unroll
             for (int db = 0; db < DB; ++db) Ak[db] = z, Av[db] = z;
             for (int qb = 0; qb < nb; ++qb) {
-                const Words16<false> at = words_of<false>(g, table, 0, qb, hf);
+                const Words16<false> at = words_of<false>(bi, ch, table, 0, qb, hf);
                 bf16x8 Aq[K / 16], Ad[K / 16];
                 read_rows<K / 16>(Aq, X + qb * 32 * XS + ako);
                 read_rows<K / 16>(Ad, Y + qb * 32 * XS + ako);
@@ -440,7 +440,7 @@ hipError_t launch_fwd_small(const Geo &g, const FwdArgs &a)
 {
     Bias bi{a.bias};
     plan_scale(g, &bi);
-    bi.w2 = 2 * g.M - 1, bi.chunk = 1, bi.rows = bi.w2;
+    plan_order(g, RIB_BF16, &bi, false);
     int windows, per, parts;
     hipError_t e = share_windows(g, &windows, &per, &parts);
     if (e != hipSuccess) return e;
@@ -457,7 +457,7 @@ hipError_t launch_bwd_small_one(const Geo &g, const BwdArgs &a, Ws &ws)
 {
     Bias bi{a.bias};
     plan_scale(g, &bi);
-    bi.w2 = 2 * g.M - 1, bi.chunk = 1, bi.rows = bi.w2;
+    plan_order(g, RIB_BF16, &bi, false);
     int windows, per, parts;
     hipError_t e = share_windows(g, &windows, &per, &parts);
     if (e != hipSuccess) return e;
@@ -483,22 +483,28 @@ template <int KX, int DB, bool SUM, int SRC>
 hipError_t launch_fwd_src(const Geo &g, const FwdArgs &a)
 {
     if (g.N <= 64) return launch_fwd_small<KX, DB, SUM, SRC>(g, a);
+    const int waves = group_waves(RIB_BF16, g.N);
     if constexpr (SRC == kFast) {
-        if (carries(g)) return launch_fwd_one<KX, DB, SUM, SRC, true, true, 4>(g, a);
-        if (g.M % 8 == 0) return launch_fwd_one<KX, DB, SUM, SRC, true, false, 4>(g, a);
+        if (strip_shift(RIB_BF16, g.M) >= 0)
+            return waves == 3 ? launch_fwd_one<KX, DB, SUM, SRC, true, 3>(g, a) : launch_fwd_one<KX, DB, SUM, SRC, true, 4>(g, a);
     }
-    return launch_fwd_one<KX, DB, SUM, SRC, false, false, 4>(g, a);
+    return waves == 2   ? launch_fwd_one<KX, DB, SUM, SRC, false, 2>(g, a)
+           : waves == 3 ? launch_fwd_one<KX, DB, SUM, SRC, false, 3>(g, a)
+                        : launch_fwd_one<KX, DB, SUM, SRC, false, 4>(g, a);
 }
 
 template <int K, int DB, int SRC, int SG>
 hipError_t launch_bwd_src(const Geo &g, const BwdArgs &a, Ws &ws)
 {
     if (g.N <= 64) return launch_bwd_small<K, DB, SRC, SG>(g, a, ws);
+    const int waves = group_waves(RIB_BF16, g.N);
     if constexpr (SG == kFast) {
-        if (carries(g)) return launch_pair<K, DB, SRC, SG, true, true, 4>(g, a, ws);
-        if (g.M % 8 == 0) return launch_pair<K, DB, SRC, SG, true, false, 4>(g, a, ws);
+        if (strip_shift(RIB_BF16, g.M) >= 0)
+            return waves == 3 ? launch_pair<K, DB, SRC, SG, true, 3>(g, a, ws) : launch_pair<K, DB, SRC, SG, true, 4>(g, a, ws);
     }
-    return launch_pair<K, DB, SRC, SG, false, false, 4>(g, a, ws);
+    return waves == 2   ? launch_pair<K, DB, SRC, SG, false, 2>(g, a, ws)
+           : waves == 3 ? launch_pair<K, DB, SRC, SG, false, 3>(g, a, ws)
+                        : launch_pair<K, DB, SRC, SG, false, 4>(g, a, ws);
 }
 template <int K, int DB, int SG>
 hipError_t launch_bwd(const Geo &g, const BwdArgs &a, Ws &ws)

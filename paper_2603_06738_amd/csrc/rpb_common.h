@@ -24,10 +24,41 @@ struct Bias {
     int chunk;              // tiles a chunk
     int rows;               // bias rows in LDS at most
     int hrows;              // rows of a wave's histogram at most
+    int prows;              // rows of a workgroup's sums at most
     // Logits in the products' own unit, q.k + bias / scale: `qs` is what q is multiplied by first (1: as it is), `bs` the
     // bias, and `c` brings a sum to base 2.  `ks`: what dS q is multiplied by.
     float qs, bs, c, ks;
+    // Strips: 2^sh columns, `strip` tokens each (a multiple of 64); sh < 0: rows of the whole window.
+    int sh, strip;
+    int sw, ws;             // columns of a strip, offsets of a row in LDS: 2 sw - 1
+    uint32_t inv_strip, inv_ws;     // n / strip == mulhi(n, inv_strip)
 };
+// Waves a workgroup: 4, or 3 or 2 where that leaves fewer of them idle at a window's end; 1 where one holds the window.
+constexpr int wave_tokens(int dtype) { return dtype == RIB_BF16 ? 64 : 32; }
+constexpr int group_waves(int dtype, int N)
+{
+    const int nb = (N + wave_tokens(dtype) - 1) / wave_tokens(dtype);
+    if (nb == 1) return 1;
+    if (dtype != RIB_BF16) return 4;
+    return nb == 2 ? 2 : (nb + 2) / 3 * 3 < (nb + 3) / 4 * 4 ? 3 : 4;
+}
+constexpr int group_tokens(int dtype, int N) { return group_waves(dtype, N) * wave_tokens(dtype); }
+// Whether windows of this side are walked in strips, and of how many columns (a power of two): where workgroups do not cross them.
+inline int strip_shift(int dtype, int M)
+{
+    const int sh = M % 32 == 0 ? 5 : M % 16 == 0 ? 4 : M % 8 == 0 ? 3 : -1;
+    return sh >= 0 && (M << sh == M * M || (M << sh) % group_tokens(dtype, M * M) == 0) ? sh : -1;
+}
+inline void plan_order(const Geo &g, int dtype, Bias *b, bool strips)
+{
+    auto inverse = [](int n) { return n > 1 ? (uint32_t)((((uint64_t)1 << 32) + n - 1) / n) : 0xffffffffu; };
+    b->w2 = 2 * g.M - 1;
+    b->sh = strips ? strip_shift(dtype, g.M) : -1;
+    b->sw = b->sh < 0 ? g.M : 1 << b->sh;
+    b->strip = g.M * b->sw;
+    b->ws = 2 * b->sw - 1;
+    b->inv_strip = inverse(b->strip), b->inv_ws = inverse(b->ws);
+}
 // Scales that are no ordinary positive number go into q (rounded to its type), so that neither bias / scale nor
 // an excluded pair's minus infinity comes out wrong.
 inline void plan_scale(const Geo &g, Bias *b)
@@ -40,31 +71,65 @@ inline void plan_scale(const Geo &g, Bias *b)
 }
 
 // The most window rows that `len` tokens from a multiple of `len` on touch.
-inline int most_rows(int len, int N, int M)
+inline int most_rows(int len, const Geo &g, const Bias &b)
 {
-    if (len >= N) return M;
-    const int rows = len % M == 0 ? len / M : M % len == 0 ? 1 : (len + M - 2) / M + 1;
-    return rows < M ? rows : M;
+    if (len >= g.N) return g.M;
+    if (b.sh >= 0) return b.strip % len == 0 ? len >> b.sh : g.M;
+    const int rows = len % g.M == 0 ? len / g.M : g.M % len == 0 ? 1 : (len + g.M - 2) / g.M + 1;
+    return rows < g.M ? rows : g.M;
 }
 
-// The bias rows of one chunk: window rows [sy0, sy1] stationary, [ty0, ty1] streamed.
-struct Chunk {
-    int ty0, ty1, c0, count;            // `count`: offsets
-};
 __device__ __forceinline__ int row_of(int n, uint32_t inv_m) { return (int)__umulhi((uint32_t)n, inv_m); }
-__device__ __forceinline__ Chunk chunk_of(const Geo &g, const Bias &b, int t0, int t1, int sy0, int sy1)
+// The n-th token of the walk: its row and column.
+struct Cell {
+    int y, x, xl;           // (xl: column in its strip)
+    __device__ __forceinline__ int lin(const Bias &b) const { return y * b.ws + xl; }
+    __device__ __forceinline__ int index(const Geo &g) const { return y * g.M + x; }       // its number in the window, as lse has it
+};
+template <bool STRIPS>
+__device__ __forceinline__ Cell cell_of(const Geo &g, const Bias &b, int n)
+{
+    Cell c;
+    if (STRIPS) {
+        const int s = (int)__umulhi((uint32_t)n, b.inv_strip), r = n - s * b.strip;
+        c.y = r >> b.sh, c.xl = r & (b.sw - 1), c.x = (s << b.sh) + c.xl;
+    } else {
+        c.y = row_of(n, g.inv_m), c.x = c.xl = n - c.y * g.M;
+    }
+    return c;
+}
+// The window rows of tokens [first, last] of one strip, and the strip's first column.
+struct Span {
+    int y0, y1, x0;
+};
+template <bool STRIPS>
+__device__ __forceinline__ Span span_of(const Geo &g, const Bias &b, int first, int last)
+{
+    const Cell c = cell_of<STRIPS>(g, b, first);
+    return Span{c.y, cell_of<STRIPS>(g, b, last).y, c.x - c.xl};
+}
+
+// The offsets of one chunk: rows `s` stationary, `t` streamed.
+struct Chunk {
+    Span s, t;
+    int c0, count;          // `count`: offsets
+    int t0;                 // first token of the streamed strip
+};
+template <bool STRIPS>
+__device__ __forceinline__ Chunk chunk_of(const Geo &g, const Bias &b, int t0, int t1, const Span &s)
 {
     Chunk c;
     const int e = t1 * kTile < g.N ? t1 * kTile : g.N;
-    c.ty0 = row_of(t0 * kTile, g.inv_m);
-    c.ty1 = row_of(e - 1, g.inv_m);
-    c.c0 = (sy1 - c.ty0) * b.w2 + g.M - 1;
-    c.count = (c.ty1 - c.ty0 + sy1 - sy0 + 1) * b.w2;
+    c.s = s, c.t = span_of<STRIPS>(g, b, t0 * kTile, e - 1);
+    c.c0 = (s.y1 - c.t.y0) * b.ws + b.sw - 1;
+    c.count = (c.t.y1 - c.t.y0 + s.y1 - s.y0 + 1) * b.ws;
+    c.t0 = STRIPS ? c.t.x0 * g.M : 0;
     return c;
 }
+
 __device__ __forceinline__ int lin(const Geo &g, int n) { return n + row_of(n, g.inv_m) * (g.M - 1); }
 
-// Whether some key is not excluded for query n; asked by whole waves.
+// Whether some key is not excluded for query n (numbered as in lse); asked by whole waves.
 __device__ __forceinline__ bool has_key(const Geo &g, const Bias &b, int hd, int n)
 {
     const float *row = b.bias + (int64_t)hd * b.w2 * b.w2 + 2 * g.M * (g.M - 1) + lin(g, n);
@@ -90,34 +155,43 @@ template <int SGN>
 __device__ __forceinline__ void stage_bias(const Geo &g, const Bias &b, const Chunk &c, int hd, float scale, float *lds, int nt)
 {
     const float *src = b.bias + (int64_t)hd * b.w2 * b.w2;
-    const int at = 2 * g.M * (g.M - 1) - SGN * c.c0;
+    // word (row, column) is row + t.y0 - s.y1 rows and column + t.x0 - s.x0 - (sw - 1) columns from stationary to streamed
+    const int at = 2 * g.M * (g.M - 1) + SGN * ((c.t.y0 - c.s.y1) * b.w2 + c.t.x0 - c.s.x0 - (b.sw - 1));
     for (int l = threadIdx.x; l < c.count; l += nt) {
-        const float x = src[at + SGN * l];
+        const int r = (int)__umulhi((uint32_t)l, b.inv_ws);
+        const float x = src[at + SGN * (l + r * (b.w2 - b.ws))];
         lds[l] = x <= kExcluded ? -INFINITY : x * scale;
     }
 }
 
 // Adds the waves' histograms of a chunk (dS summed by offset, `hsize` values a wave, WT stationary tokens each) in their order, writes
-// them to the workgroup's sums `dst` (from the chunk's first row on) and clears them.  `before`: the last streamed row of the chunk
-// before (-1: none); rows which that one touched are added to.
-template <int W, int WT>
-__device__ __forceinline__ void flush(const Geo &g, const Bias &b, const Chunk &ch, double *H, int hsize, int first, int sy0, int sy1, int before, float *dst)
+// them to the workgroup's sums `dst` (of this streamed strip, from the chunk's first row on) and clears them.  `before`: the last row of
+// the strip's chunk before (-1: none); what that one touched is added to.
+template <bool STRIPS, int W, int WT>
+__device__ __forceinline__ void flush(const Geo &g, const Bias &b, const Chunk &ch, double *H, int hsize, int first, int before, float *dst)
 {
-    const int old = before < 0 ? 0 : (before - ch.ty0 + sy1 - sy0 + 1) * b.w2;
+    const int old = before < 0 ? 0 : (before - ch.t.y0 + ch.s.y1 - ch.s.y0 + 1) * b.ws;
     for (int e = threadIdx.x; e < ch.count; e += 64 * W) {
         double sum = 0.;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            const int f = first + w * WT, l = f + WT < g.N ? f + WT - 1 : g.N - 1;
+            const int f = first + w * WT;
             if (f >= g.N) break;
-            const int y0 = row_of(f, g.inv_m), y1 = row_of(l, g.inv_m), at = e - (sy1 - y1) * b.w2;
-            if (at >= 0 && at < (ch.ty1 - ch.ty0 + y1 - y0 + 1) * b.w2) {
+            const Span v = span_of<STRIPS>(g, b, f, f + WT < g.N ? f + WT - 1 : g.N - 1);
+            const int at = e - (ch.s.y1 - v.y1) * b.ws;
+            if (at >= 0 && at < (ch.t.y1 - ch.t.y0 + v.y1 - v.y0 + 1) * b.ws) {
                 sum += H[w * hsize + at];
                 H[w * hsize + at] = 0.;
             }
         }
         dst[e] = (float)(e < old ? sum + dst[e] : sum);
     }
+}
+// The place of a workgroup's sums: [unit][workgroup][streamed strip][prows][ws].
+__device__ __forceinline__ int64_t sums_at(const Geo &g, const Bias &b, int64_t u, int nblk, int blk, int prows, int x0)
+{
+    const int n = b.sh < 0 ? 1 : g.M >> b.sh;
+    return (((u * nblk + blk) * n + (b.sh < 0 ? 0 : x0 >> b.sh)) * prows) * b.ws;
 }
 
 // ---- sources of rows ---------------------------------------------------------------------------------------------
@@ -165,41 +239,47 @@ hipError_t launch_unpack(const Geo &g, int dtype, const uint8_t *ckpt, void *q, 
 struct Ws {
     size_t ext, part, total;
     int nblk;                           // workgroups a unit
-    int prows;                          // rows of a workgroup's sums
+    int words;                          // of a workgroup's sums at most
+    bool strips;                        // how the first kernel walked the windows
     int shares;                         // sums a head: of windows, or of the runs of windows a wave takes
 };
-// Stationary tokens of a wave, and of a workgroup.
-constexpr int wave_tokens(int dtype) { return dtype == RIB_BF16 ? 64 : 32; }
-constexpr int group_tokens(int dtype, int N) { return N <= wave_tokens(dtype) ? wave_tokens(dtype) : 4 * wave_tokens(dtype); }
 inline Ws ws_layout(const Geo &g, int dtype)
 {
     Ws w;
     const int sb = group_tokens(dtype, g.N);
     w.nblk = (g.N + sb - 1) / sb;
-    w.prows = g.M - 1 + most_rows(sb, g.N, g.M);
-    auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+    w.words = 0;
+    for (int strips = 0; strips < 2; ++strips) {        // (which way depends on the tensors' alignment too)
+        Bias b{};
+        plan_order(g, dtype, &b, strips != 0);
+        const int prows = g.M - 1 + most_rows(sb, g, b), words = (b.sh < 0 ? 1 : g.M >> b.sh) * prows * b.ws;
+        if (words > w.words) w.words = words;
+    }
+    w.strips = false;
     w.shares = (int)(g.units / g.heads);
+    auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     w.ext = 0;
     w.part = up((size_t)g.units * g.N * 8);
-    w.total = w.part + up((size_t)g.units * w.nblk * w.prows * (2 * g.M - 1) * sizeof(float));
+    w.total = w.part + up((size_t)g.units * w.nblk * w.words * sizeof(float));
     return w;
 }
 // dbias[head][offset] from the workgroups' sums: windows and workgroups in a fixed order.
 hipError_t launch_reduce(const Geo &g, int dtype, const Ws &w, const float *part, float *dbias, hipStream_t st);
 
-// Tiles a chunk and the rows that go with it: as many tiles as fit `bias_bytes` of bias and (hist) `hist_bytes` a wave.
-inline void plan_chunks(const Geo &g, int dtype, Bias *b, bool hist, size_t bias_bytes, size_t hist_bytes)
+// Tiles a chunk and the rows that go with it: as many tiles as fit `bias_bytes` of bias and (hist) `hist_bytes` a wave, of one strip.
+inline void plan_chunks(const Geo &g, int dtype, Bias *b, bool strips, bool hist, size_t bias_bytes, size_t hist_bytes)
 {
-    const int sb = group_tokens(dtype, g.N), ntiles = (g.N + kTile - 1) / kTile;
-    const int srows = most_rows(sb, g.N, g.M), wrows = most_rows(wave_tokens(dtype), g.N, g.M);
-    b->w2 = 2 * g.M - 1;
-    int tiles = ntiles;
-    for (;; tiles = tiles > 8 ? tiles - tiles / 8 : tiles - 1) {
-        const int trows = most_rows(tiles * kTile, g.N, g.M);
+    plan_order(g, dtype, b, strips);
+    const int sb = group_tokens(dtype, g.N), ntiles = (b->strip + kTile - 1) / kTile;
+    const int srows = most_rows(sb, g, *b), wrows = most_rows(wave_tokens(dtype), g, *b);
+    b->prows = g.M - 1 + srows;
+    for (int tiles = ntiles;; tiles = tiles > 8 ? tiles - tiles / 8 : tiles - 1) {
+        // (a strip's chunks start at multiples of `tiles` from its start)
+        const int trows = b->sh >= 0 ? tiles * kTile >> b->sh : most_rows(tiles * kTile, g, *b);
         b->chunk = tiles;
         b->rows = trows + srows - 1;
         b->hrows = hist ? trows + wrows - 1 : 0;
-        const bool fits = (size_t)b->rows * b->w2 * 4 <= bias_bytes && (size_t)b->hrows * b->w2 * 8 <= hist_bytes;
+        const bool fits = (size_t)b->rows * b->ws * 4 <= bias_bytes && (size_t)b->hrows * b->ws * 8 <= hist_bytes;
         if (fits || tiles == 1) return;
     }
 }

@@ -61,28 +61,29 @@ __device__ __forceinline__ Raw get4(const Rows &s, uint32_t t, int n, int c, int
     }
 }
 
-template <int DB, int W, bool CX, bool CY, bool EXT>
+template <int DB, int W, bool CX, bool CY, bool EXT, bool ALN>
 struct Mover {
     static constexpr int LP = 8 * DB, NT = 64 * W, P = (kTile * LP + NT - 1) / NT;
     Raw x[P], y[P];
     float2 e;
 
-    __device__ __forceinline__ void request(const Geo &g, const Win &win, const Rows &xs, const Rows &ys, const float2 *ext, int tile)
+    __device__ __forceinline__ void request(const Geo &g, const Bias &bi, const Win &win, const Rows &xs, const Rows &ys, const float2 *ext, int tile)
     {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const int slot = p * NT + threadIdx.x, row = slot / LP, j = slot % LP;
             const int n0 = tile * kTile + row, n = n0 < g.N ? n0 : g.N - 1;
-            const uint32_t t = CX && CY ? 0u : pixel(win, n);
-            x[p] = get4<CX>(xs, t, n, 4 * j, g.d);
-            y[p] = get4<CY>(ys, t, n, 4 * j, g.d);
+            const Cell c = cell_of<ALN>(g, bi, n);
+            const uint32_t t = CX && CY ? 0u : pixel(win, c);
+            x[p] = get4<CX>(xs, t, c.index(g), 4 * j, g.d);
+            y[p] = get4<CY>(ys, t, c.index(g), 4 * j, g.d);
         }
         if (EXT && threadIdx.x < kTile) {
             const int n = tile * kTile + threadIdx.x;
             e = n < g.N ? ext[n] : float2{-bf::kNoRow, 0.f};
         }
     }
-    __device__ __forceinline__ void commit(const Geo &g, float *S, int tile, float scale)
+    __device__ __forceinline__ void commit(const Geo &g, const Bias &bi, float *S, int tile, float scale)
     {
         using I = Img<DB>;
 #pragma unroll
@@ -96,7 +97,7 @@ struct Mover {
         }
         if (threadIdx.x < kTile) {
             const int n = tile * kTile + threadIdx.x;
-            ((int *)(S + I::LT))[threadIdx.x] = lin(g, n < g.N ? n : g.N - 1);
+            if (!ALN) ((int *)(S + I::LT))[threadIdx.x] = cell_of<false>(g, bi, n < g.N ? n : g.N - 1).lin(bi);
             if (EXT) S[I::EX + threadIdx.x] = e.x, S[I::EX + kTile + threadIdx.x] = e.y;
         }
     }
@@ -104,13 +105,13 @@ struct Mover {
 
 // A lane's B operands of its stationary token: channels 8 s + 4 hf .. + 3 of step s.
 template <int DB, bool CKPT>
-__device__ __forceinline__ void operand(const Geo &g, const Place &pl, const Rows &s, int n, float scale, Raw (&B)[4 * DB])
+__device__ __forceinline__ void operand(const Geo &g, const Place &pl, const Rows &s, const Cell &c, float scale, Raw (&B)[4 * DB])
 {
     const int hf = (threadIdx.x & 63) >> 5;
-    const uint32_t t = CKPT ? 0u : pixel(pl.win, n);
+    const uint32_t t = CKPT ? 0u : pixel(pl.win, c);
 #pragma unroll
     for (int k = 0; k < 4 * DB; ++k) {
-        B[k] = get4<CKPT>(s, t, n, 8 * k + 4 * hf, g.d);
+        B[k] = get4<CKPT>(s, t, c.index(g), 8 * k + 4 * hf, g.d);
         B[k].x *= scale, B[k].y *= scale, B[k].z *= scale, B[k].w *= scale;
     }
 }
@@ -166,38 +167,38 @@ __device__ __forceinline__ Rows rows_of_ckpt(const Geo &g, const Place &p, const
 
 template <bool MAX, int DB, bool ALN, int W>
 __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Place &pl, const Rows &ks, const Rows &vs, float *S, float *B,
-                                         const Raw (&Q)[4 * DB], f32x16 (&O)[DB], float &sum, float &top, int sy0, int sy1, int mylin, bool active)
+                                         const Raw (&Q)[4 * DB], f32x16 (&O)[DB], float &sum, float &top, const Span &span, int mylin, bool active)
 {
     using I = Img<DB>;
     constexpr int NT = 64 * W;
     const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5;
-    const int ntiles = (g.N + kTile - 1) / kTile;
+    const int ntiles = (g.N + kTile - 1) / kTile, strip_tiles = ALN ? bi.strip / kTile : ntiles;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) O[db][i] = 0.f;
     sum = 0.f, top = MAX ? -INFINITY : 0.f;
-    Mover<DB, W, false, false, false> mv;
-    mv.request(g, pl.win, ks, vs, nullptr, 0);
-    mv.commit(g, S, 0, 1.f);
-    mv.request(g, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
-    for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
-        const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
-        const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
+    Mover<DB, W, false, false, false, ALN> mv;
+    mv.request(g, bi, pl.win, ks, vs, nullptr, 0);
+    mv.commit(g, bi, S, 0, 1.f);
+    mv.request(g, bi, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
+    for (int t0 = 0, t1, end = strip_tiles; t0 < ntiles; t0 = t1) {
+        t1 = t0 + bi.chunk < end ? t0 + bi.chunk : end;
+        const Chunk ch = chunk_of<ALN>(g, bi, t0, t1, span);
         stage_bias<-1>(g, bi, ch, pl.hd, 1.f, B, NT);
         __syncthreads();
         for (int tile = t0; tile < t1; ++tile) {
             const float *cur = S + (tile & 1) * I::STAGE;
             if (tile + 1 < ntiles) {
-                mv.commit(g, S + ((tile + 1) & 1) * I::STAGE, tile + 1, 1.f);
-                mv.request(g, pl.win, ks, vs, nullptr, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
+                mv.commit(g, bi, S + ((tile + 1) & 1) * I::STAGE, tile + 1, 1.f);
+                mv.request(g, bi, pl.win, ks, vs, nullptr, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
             }
             if (active) {
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb) {
                     const int key0 = tile * kTile + kb * 32;
                     if (!ALN && key0 >= g.N) break;
-                    const Words16<ALN> wd = words_of<ALN>(g, (const int *)(cur + I::LT), tile, kb, hf);
+                    const Words16<ALN> wd = words_of<ALN>(bi, ch, (const int *)(cur + I::LT), tile, kb, hf);
                     f32x16 s = scores<DB>(cur + (kb * 32 + col) * I::STR + 4 * hf, Q, bias_block<ALN>(B + ch.c0 - mylin, wd), g.d);
                     if (!ALN) mask_rows(s, key0, g.N, hf);
 #pragma unroll
@@ -229,6 +230,7 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
             }
             __syncthreads();
         }
+        if (t1 == end) end += strip_tiles;
     }
     sum += __shfl_xor(sum, 32);
 }
@@ -247,10 +249,12 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void fwd_kernel(Geo g, Bias
     const Place pl = place_of(g, nblk, NT, map);
     __syncthreads();
     const int first = pl.blk * SB, last = first + SB < g.N ? first + SB - 1 : g.N - 1, n0 = first + wave * 32, n = n0 + col;
-    const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m), nc = n < g.N ? n : g.N - 1;
+    const Span span = span_of<ALN>(g, bi, first, last);
+    const int nc = n < g.N ? n : g.N - 1;
+    const Cell cell = cell_of<ALN>(g, bi, nc);
     const bool active = n0 < g.N;
     Raw Q[4 * DB];
-    operand<DB, false>(g, pl, rows_of_grid(g, pl, q, g.tstride), nc, g.scale_c, Q);
+    operand<DB, false>(g, pl, rows_of_grid(g, pl, q, g.tstride), cell, g.scale_c, Q);
     const Rows ks = rows_of_grid(g, pl, k, g.tstride), vs = rows_of_grid(g, pl, v, g.tstride);
     f32x16 O[DB];
     float sum, top;
@@ -258,19 +262,19 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void fwd_kernel(Geo g, Bias
     // workgroup on a second walk, with one.
     bool bad = true;
     if (!force_max) {
-        fwd_walk<false, DB, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, sy0, sy1, lin(g, nc), active);
-        bad = active && bad_rows(g, bi, pl.hd, n, sum);
+        fwd_walk<false, DB, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, cell.lin(bi), active);
+        bad = active && bad_rows(g, bi, pl.hd, n < g.N ? cell.index(g) : g.N, sum);
     }
-    if (__syncthreads_or(bad)) fwd_walk<true, DB, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, sy0, sy1, lin(g, nc), active);
+    if (__syncthreads_or(bad)) fwd_walk<true, DB, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, cell.lin(bi), active);
     if (n >= g.N) return;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;         // (a row without a key: zeros)
-    if (lse != nullptr && hf == 0) lse[(int64_t)pl.u * g.N + n] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
-    store_row<DB>(out + (pl.img + pixel(pl.win, n)) * g.C + pl.hd * g.d, O, g.d, hf, inv);
+    if (lse != nullptr && hf == 0) lse[(int64_t)pl.u * g.N + cell.index(g)] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    store_row<DB>(out + (pl.img + pixel(pl.win, cell)) * g.C + pl.hd * g.d, O, g.d, hf, inv);
 }
 
 // dq and the bias's gradient; the second kernel's -LSE and -delta of every row.
 template <int DB, bool CKPT, bool ALN, int W, bool HIST>
-__global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias bi, int nblk, int prows, const float *__restrict__ q,
+__global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias bi, int nblk, const float *__restrict__ q,
                                                        const float *__restrict__ k, const float *__restrict__ v,
                                                        const uint8_t *__restrict__ ckpt, const float *__restrict__ out,
                                                        const float *__restrict__ dout, const float *__restrict__ lse,
@@ -282,30 +286,32 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
     float *S = (float *)smem;
     int *map = (int *)(smem + stage_bytes<DB>());
     float *B = (float *)(map + 2 * g.M);
-    double *H = (double *)(B + ((bi.rows * bi.w2 + 1) & ~1));
-    const int hsize = bi.hrows * bi.w2;
+    double *H = (double *)(B + ((bi.rows * bi.ws + 1) & ~1));
+    const int hsize = bi.hrows * bi.ws;
     const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place pl = place_of(g, nblk, NT, map);
     if (HIST)
         for (int e = threadIdx.x; e < W * hsize; e += NT) H[e] = 0.;
     __syncthreads();
     const int first = pl.blk * SB, last = first + SB < g.N ? first + SB - 1 : g.N - 1, n0 = first + wave * 32, n = n0 + col;
-    const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m), nc = n < g.N ? n : g.N - 1;
+    const Span span = span_of<ALN>(g, bi, first, last);
+    const int nc = n < g.N ? n : g.N - 1;
+    const Cell cell = cell_of<ALN>(g, bi, nc);
     const bool active = n0 < g.N;
     Raw Q[4 * DB], D[4 * DB];
-    operand<DB, false>(g, pl, rows_of_grid(g, pl, dout, g.C), nc, 1.f, D);
+    operand<DB, false>(g, pl, rows_of_grid(g, pl, dout, g.C), cell, 1.f, D);
     float delta = 0.f;
     {
         Raw O[4 * DB];
-        operand<DB, false>(g, pl, rows_of_grid(g, pl, out, g.C), nc, 1.f, O);
+        operand<DB, false>(g, pl, rows_of_grid(g, pl, out, g.C), cell, 1.f, O);
 #pragma unroll
         for (int i = 0; i < 4 * DB; ++i) delta += (O[i].x * D[i].x + O[i].y * D[i].y) + (O[i].z * D[i].z + O[i].w * D[i].w);
         delta += __shfl_xor(delta, 32);
     }
-    operand<DB, CKPT>(g, pl, CKPT ? rows_of_ckpt(g, pl, ckpt, 0) : rows_of_grid(g, pl, q, g.tstride), nc, g.scale_c, Q);
-    const float e0 = lse[(int64_t)pl.u * g.N + nc], L = n >= g.N || e0 == -INFINITY ? bf::kNoRow : e0;
+    operand<DB, CKPT>(g, pl, CKPT ? rows_of_ckpt(g, pl, ckpt, 0) : rows_of_grid(g, pl, q, g.tstride), cell, g.scale_c, Q);
+    const float e0 = lse[(int64_t)pl.u * g.N + cell.index(g)], L = n >= g.N || e0 == -INFINITY ? bf::kNoRow : e0;
     if (n < g.N && hf == 0) ext[(int64_t)pl.u * g.N + n] = float2{-L, -delta};
-    const int mylin = lin(g, nc), wsy1 = row_of(n0 + 31 < g.N ? n0 + 31 : g.N - 1, g.inv_m);
+    const int mylin = cell.lin(bi), wsy1 = span_of<ALN>(g, bi, n0 < g.N ? n0 : g.N - 1, n0 + 31 < g.N ? n0 + 31 : g.N - 1).y1;
     const Rows ks = CKPT ? rows_of_ckpt(g, pl, ckpt, 1) : rows_of_grid(g, pl, k, g.tstride);
     const Rows vs = CKPT ? rows_of_ckpt(g, pl, ckpt, 2) : rows_of_grid(g, pl, v, g.tstride);
     f32x16 A[DB];
@@ -313,31 +319,31 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) A[db][i] = 0.f;
-    const int ntiles = (g.N + kTile - 1) / kTile;
+    const int ntiles = (g.N + kTile - 1) / kTile, strip_tiles = ALN ? bi.strip / kTile : ntiles;
     const f32x16 z = {0};
-    Mover<DB, W, CKPT, CKPT, false> mv;
-    mv.request(g, pl.win, ks, vs, nullptr, 0);
-    mv.commit(g, S, 0, 1.f);
-    mv.request(g, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
+    Mover<DB, W, CKPT, CKPT, false, ALN> mv;
+    mv.request(g, bi, pl.win, ks, vs, nullptr, 0);
+    mv.commit(g, bi, S, 0, 1.f);
+    mv.request(g, bi, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
     int before = -1;
-    for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
-        const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
-        const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
+    for (int t0 = 0, t1, end = strip_tiles; t0 < ntiles; t0 = t1) {
+        t1 = t0 + bi.chunk < end ? t0 + bi.chunk : end;
+        const Chunk ch = chunk_of<ALN>(g, bi, t0, t1, span);
         stage_bias<-1>(g, bi, ch, pl.hd, 1.f, B, NT);
-        double *const mine = H + wave * hsize + ch.c0 - (sy1 - wsy1) * bi.w2 - mylin;
+        double *const mine = H + wave * hsize + ch.c0 - (span.y1 - wsy1) * bi.ws - mylin;
         __syncthreads();
         for (int tile = t0; tile < t1; ++tile) {
             const float *cur = S + (tile & 1) * I::STAGE;
             if (tile + 1 < ntiles) {
-                mv.commit(g, S + ((tile + 1) & 1) * I::STAGE, tile + 1, 1.f);
-                mv.request(g, pl.win, ks, vs, nullptr, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
+                mv.commit(g, bi, S + ((tile + 1) & 1) * I::STAGE, tile + 1, 1.f);
+                mv.request(g, bi, pl.win, ks, vs, nullptr, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
             }
             if (active) {
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb) {
                     const int key0 = tile * kTile + kb * 32;
                     if (!ALN && key0 >= g.N) break;
-                    const Words16<ALN> wd = words_of<ALN>(g, (const int *)(cur + I::LT), tile, kb, hf);
+                    const Words16<ALN> wd = words_of<ALN>(bi, ch, (const int *)(cur + I::LT), tile, kb, hf);
                     const float *row = cur + (kb * 32 + col) * I::STR + 4 * hf;
                     f32x16 s = scores<DB>(row, Q, bias_block<ALN>(B + ch.c0 - mylin, wd), g.d);
                     const f32x16 p = scores<DB>(row + I::YR, D, z, g.d);
@@ -355,13 +361,14 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
             __syncthreads();
         }
         if (HIST) {
-            flush<W, 32>(g, bi, ch, H, hsize, first, sy0, sy1, before,
-                         part + ((int64_t)pl.u * nblk + pl.blk) * prows * bi.w2 + ch.ty0 * bi.w2);
-            before = ch.ty1;
+            flush<ALN, W, 32>(g, bi, ch, H, hsize, first, before,
+                              part + sums_at(g, bi, pl.u, nblk, pl.blk, bi.prows, ch.t.x0) + ch.t.y0 * bi.ws);
+            before = t1 == end ? -1 : ch.t.y1;
         }
+        if (t1 == end) end += strip_tiles;
     }
     if (n >= g.N) return;
-    store_row<DB>(dq + (pl.img + pixel(pl.win, n)) * g.C + pl.hd * g.d, A, g.d, hf, g.scale_c);
+    store_row<DB>(dq + (pl.img + pixel(pl.win, cell)) * g.C + pl.hd * g.d, A, g.d, hf, g.scale_c);
 }
 
 template <int DB, bool CKPT, bool ALN, int W>
@@ -380,12 +387,14 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
     const Place pl = place_of(g, nblk, NT, map);
     __syncthreads();
     const int first = pl.blk * SB, last = first + SB < g.N ? first + SB - 1 : g.N - 1, n0 = first + wave * 32, n = n0 + col;
-    const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m), nc = n < g.N ? n : g.N - 1;
+    const Span span = span_of<ALN>(g, bi, first, last);
+    const int nc = n < g.N ? n : g.N - 1;
+    const Cell cell = cell_of<ALN>(g, bi, nc);
     const bool active = n0 < g.N;
     Raw Kb[4 * DB], Vb[4 * DB];
-    operand<DB, CKPT>(g, pl, CKPT ? rows_of_ckpt(g, pl, ckpt, 1) : rows_of_grid(g, pl, k, g.tstride), nc, 1.f, Kb);
-    operand<DB, CKPT>(g, pl, CKPT ? rows_of_ckpt(g, pl, ckpt, 2) : rows_of_grid(g, pl, v, g.tstride), nc, 1.f, Vb);
-    const int mylin = lin(g, nc);
+    operand<DB, CKPT>(g, pl, CKPT ? rows_of_ckpt(g, pl, ckpt, 1) : rows_of_grid(g, pl, k, g.tstride), cell, 1.f, Kb);
+    operand<DB, CKPT>(g, pl, CKPT ? rows_of_ckpt(g, pl, ckpt, 2) : rows_of_grid(g, pl, v, g.tstride), cell, 1.f, Vb);
+    const int mylin = cell.lin(bi);
     const Rows qs = CKPT ? rows_of_ckpt(g, pl, ckpt, 0) : rows_of_grid(g, pl, q, g.tstride), ds = rows_of_grid(g, pl, dout, g.C);
     const float2 *const ex = ext + (int64_t)pl.u * g.N;
     f32x16 Ak[DB], Av[DB];
@@ -393,29 +402,29 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) Ak[db][i] = 0.f, Av[db][i] = 0.f;
-    const int ntiles = (g.N + kTile - 1) / kTile;
+    const int ntiles = (g.N + kTile - 1) / kTile, strip_tiles = ALN ? bi.strip / kTile : ntiles;
     const float scale = g.scale_c;
     const f32x16 z = {0};
-    Mover<DB, W, CKPT, false, true> mv;
-    mv.request(g, pl.win, qs, ds, ex, 0);
-    mv.commit(g, S, 0, scale);
-    mv.request(g, pl.win, qs, ds, ex, ntiles > 1 ? 1 : 0);
-    for (int t0 = 0; t0 < ntiles; t0 += bi.chunk) {
-        const int t1 = t0 + bi.chunk < ntiles ? t0 + bi.chunk : ntiles;
-        const Chunk ch = chunk_of(g, bi, t0, t1, sy0, sy1);
+    Mover<DB, W, CKPT, false, true, ALN> mv;
+    mv.request(g, bi, pl.win, qs, ds, ex, 0);
+    mv.commit(g, bi, S, 0, scale);
+    mv.request(g, bi, pl.win, qs, ds, ex, ntiles > 1 ? 1 : 0);
+    for (int t0 = 0, t1, end = strip_tiles; t0 < ntiles; t0 = t1) {
+        t1 = t0 + bi.chunk < end ? t0 + bi.chunk : end;
+        const Chunk ch = chunk_of<ALN>(g, bi, t0, t1, span);
         stage_bias<1>(g, bi, ch, pl.hd, 1.f, B, NT);
         __syncthreads();
         for (int tile = t0; tile < t1; ++tile) {
             const float *cur = S + (tile & 1) * I::STAGE;
             if (tile + 1 < ntiles) {
-                mv.commit(g, S + ((tile + 1) & 1) * I::STAGE, tile + 1, scale);
-                mv.request(g, pl.win, qs, ds, ex, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
+                mv.commit(g, bi, S + ((tile + 1) & 1) * I::STAGE, tile + 1, scale);
+                mv.request(g, bi, pl.win, qs, ds, ex, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
             }
             if (active) {
 #pragma unroll
                 for (int qb = 0; qb < 2; ++qb) {
                     if (!ALN && tile * kTile + qb * 32 >= g.N) break;
-                    const Words16<ALN> wd = words_of<ALN>(g, (const int *)(cur + I::LT), tile, qb, hf);
+                    const Words16<ALN> wd = words_of<ALN>(bi, ch, (const int *)(cur + I::LT), tile, qb, hf);
                     const float *row = cur + (qb * 32 + col) * I::STR + 4 * hf;
                     f32x16 s = scores<DB>(row, Kb, bias_block<ALN>(B + ch.c0 - mylin, wd), g.d), p = scores<DB>(row + I::YR, Vb, z, g.d);
                     // (LSE and delta only then: sums that start from them would round at their size)
@@ -435,9 +444,10 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
             }
             __syncthreads();
         }
+        if (t1 == end) end += strip_tiles;
     }
     if (n >= g.N) return;
-    const int64_t at = (pl.img + pixel(pl.win, n)) * g.C + pl.hd * g.d;
+    const int64_t at = (pl.img + pixel(pl.win, cell)) * g.C + pl.hd * g.d;
     store_row<DB>(dk + at, Ak, g.d, hf, 1.f);           // (Q carries the scale)
     store_row<DB>(dv + at, Av, g.d, hf, 1.f);
 }
@@ -448,9 +458,9 @@ template <int DB, bool ALN, int W>
 hipError_t launch_fwd_one(const Geo &g, const FwdArgs &a)
 {
     Bias bi{a.bias};
-    plan_chunks(g, RIB_F32, &bi, false, kBiasBytes, 0);
+    plan_chunks(g, RIB_F32, &bi, ALN, false, kBiasBytes, 0);
     const int nblk = (g.N + 32 * W - 1) / (32 * W);
-    const size_t smem = stage_bytes<DB>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.w2 * 4;
+    const size_t smem = stage_bytes<DB>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.ws * 4;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
     auto kern = fwd_kernel<DB, ALN, W>;
     const hipError_t e = prepare_kernel((const void *)kern, nullptr);
@@ -463,32 +473,33 @@ template <int DB>
 hipError_t launch_fwd_width(const Geo &g, const FwdArgs &a)
 {
     if (g.N <= 32) return launch_fwd_one<DB, false, 1>(g, a);
-    return g.M % 8 == 0 ? launch_fwd_one<DB, true, 4>(g, a) : launch_fwd_one<DB, false, 4>(g, a);
+    return strip_shift(RIB_F32, g.M) >= 0 ? launch_fwd_one<DB, true, 4>(g, a) : launch_fwd_one<DB, false, 4>(g, a);
 }
 
 template <int DB, bool CKPT, bool ALN, int W, bool HIST>
 hipError_t launch_dq_one(const Geo &g, const BwdArgs &a, const Ws &ws)
 {
     Bias bi{a.bias};
-    plan_chunks(g, RIB_F32, &bi, HIST, kBiasBytes, kHistBytes);
-    const size_t smem = stage_bytes<DB>() + 8 * (size_t)g.M + ((size_t)bi.rows * bi.w2 + 1) / 2 * 8 + (size_t)W * bi.hrows * bi.w2 * 8;
+    plan_chunks(g, RIB_F32, &bi, ALN, HIST, kBiasBytes, kHistBytes);
+    const size_t smem = stage_bytes<DB>() + 8 * (size_t)g.M + ((size_t)bi.rows * bi.ws + 1) / 2 * 8 + (size_t)W * bi.hrows * bi.ws * 8;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
     auto kern = dq_kernel<DB, CKPT, ALN, W, HIST>;
     const hipError_t e = prepare_kernel((const void *)kern, nullptr);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * ws.nblk)), dim3(64 * W), smem, a.st, g, bi, ws.nblk, ws.prows, (const float *)a.q,
+    hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * ws.nblk)), dim3(64 * W), smem, a.st, g, bi, ws.nblk, (const float *)a.q,
                        (const float *)a.k, (const float *)a.v, a.ckpt, (const float *)a.out, (const float *)a.dout, a.lse, (float *)a.dq,
                        (float2 *)((char *)a.ws + ws.ext), (float *)((char *)a.ws + ws.part));
     return hipGetLastError();
 }
 template <int DB, bool CKPT, bool ALN, int W>
-hipError_t launch_pair(const Geo &g, const BwdArgs &a, const Ws &ws)
+hipError_t launch_pair(const Geo &g, const BwdArgs &a, Ws &ws)
 {
+    ws.strips = ALN;
     hipError_t e = a.dbias != nullptr ? launch_dq_one<DB, CKPT, ALN, W, true>(g, a, ws) : launch_dq_one<DB, CKPT, ALN, W, false>(g, a, ws);
     if (e != hipSuccess) return e;
     Bias bi{a.bias};
-    plan_chunks(g, RIB_F32, &bi, false, kBiasBytes, 0);
-    const size_t smem = stage_bytes<DB>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.w2 * 4;
+    plan_chunks(g, RIB_F32, &bi, ALN, false, kBiasBytes, 0);
+    const size_t smem = stage_bytes<DB>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.ws * 4;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
     auto kern = dkv_kernel<DB, CKPT, ALN, W>;
     e = prepare_kernel((const void *)kern, nullptr);
@@ -499,13 +510,13 @@ hipError_t launch_pair(const Geo &g, const BwdArgs &a, const Ws &ws)
     return hipGetLastError();
 }
 template <int DB, bool CKPT>
-hipError_t launch_bwd_src(const Geo &g, const BwdArgs &a, const Ws &ws)
+hipError_t launch_bwd_src(const Geo &g, const BwdArgs &a, Ws &ws)
 {
     if (g.N <= 32) return launch_pair<DB, CKPT, false, 1>(g, a, ws);
-    return g.M % 8 == 0 ? launch_pair<DB, CKPT, true, 4>(g, a, ws) : launch_pair<DB, CKPT, false, 4>(g, a, ws);
+    return strip_shift(RIB_F32, g.M) >= 0 ? launch_pair<DB, CKPT, true, 4>(g, a, ws) : launch_pair<DB, CKPT, false, 4>(g, a, ws);
 }
 template <int DB>
-hipError_t launch_bwd_width(const Geo &g, const BwdArgs &a, const Ws &ws)
+hipError_t launch_bwd_width(const Geo &g, const BwdArgs &a, Ws &ws)
 {
     return a.ckpt != nullptr ? launch_bwd_src<DB, true>(g, a, ws) : launch_bwd_src<DB, false>(g, a, ws);
 }
@@ -519,7 +530,7 @@ hipError_t launch_fwd_f32(const Geo &g, const FwdArgs &a)
 
 hipError_t launch_bwd_f32(const Geo &g, const BwdArgs &a)
 {
-    const Ws ws = ws_layout(g, RIB_F32);
+    Ws ws = ws_layout(g, RIB_F32);
     const hipError_t e = g.d <= 32 ? fp::launch_bwd_width<1>(g, a, ws) : fp::launch_bwd_width<2>(g, a, ws);
     if (e != hipSuccess || a.dbias == nullptr) return e;
     return launch_reduce(g, RIB_F32, ws, (const float *)((const char *)a.ws + ws.part), a.dbias, a.st);

@@ -80,25 +80,30 @@ __global__ __launch_bounds__(1024) void table_bwd_kernel(int L, int buckets, int
 
 // dbias[head][o] = sum over windows and their workgroups of the workgroups' sums.  64 offsets a workgroup, 16 threads an offset: up to 16 runs
 // of windows, the rest of the 16 over a window's workgroups, then the 16 in a fixed order.  Bound by memory: every partial sum is read once.
-__global__ __launch_bounds__(1024) void reduce_kernel(Geo g, int windows, int runs, int nblk, int prows, int group, const float *__restrict__ part,
+__global__ __launch_bounds__(1024) void reduce_kernel(Geo g, Bias bi, int windows, int runs, int nblk, int group, const float *__restrict__ part,
                                                       float *__restrict__ dbias)
 {
     __shared__ float run[16][64];
-    const int w2 = 2 * g.M - 1, L = w2 * w2, hd = blockIdx.y, size = prows * w2;
+    const int L = bi.w2 * bi.w2, hd = blockIdx.y, strips = bi.sh < 0 ? 1 : g.M >> bi.sh, size = strips * bi.prows * bi.ws;
     const int lane = threadIdx.x & 63, r = threadIdx.x >> 6, o = blockIdx.x * 64 + lane, rw = r % runs;
     const int per = (windows + runs - 1) / runs, w0 = rw * per, w1 = w0 + per < windows ? w0 + per : windows;
     const int64_t step = (int64_t)g.heads * nblk * size;
+    // from stationary to streamed, a query to a key, is minus the offset
+    const int oy = o / bi.w2, dy = g.M - 1 - oy, dx = g.M - 1 - (o - oy * bi.w2);
     float sum = 0.f;
     if (o < L)
         for (int blk = r / runs; blk < nblk; blk += 16 / runs) {
             const int first = blk * group, last = first + group < g.N ? first + group - 1 : g.N - 1;
-            const int sy0 = row_of(first, g.inv_m), sy1 = row_of(last, g.inv_m);
-            // the offset's word of a workgroup's rows (streamed - stationary row, from -sy1 on, is minus the offset's)
-            const int at = 2 * g.M * (g.M - 1) + sy1 * w2 + g.M - 1 - o;
-            if (at < 0 || at >= (g.M + sy1 - sy0) * w2) continue;
-            const float *p = part + ((int64_t)w0 * g.heads + hd) * nblk * size + (int64_t)blk * size + at;
+            const Span v = bi.sh >= 0 ? span_of<true>(g, bi, first, last) : span_of<false>(g, bi, first, last);
+            const int row = dy + v.y1;
+            if (row < 0 || row >= g.M + v.y1 - v.y0) continue;
+            for (int s = 0; s < strips; ++s) {
+                const int c = dx + v.x0 - s * bi.sw + bi.sw - 1;
+                if (c < 0 || c >= bi.ws) continue;
+                const float *p = part + sums_at(g, bi, (int64_t)w0 * g.heads + hd, nblk, blk, bi.prows, s * bi.sw) + row * bi.ws + c;
 #pragma unroll 8
-            for (int w = w0; w < w1; ++w, p += step) sum += *p;
+                for (int w = w0; w < w1; ++w, p += step) sum += *p;
+            }
         }
     run[r][lane] = sum;
     __syncthreads();
@@ -113,10 +118,13 @@ __global__ __launch_bounds__(1024) void reduce_kernel(Geo g, int windows, int ru
 hipError_t launch_reduce(const Geo &g, int dtype, const Ws &w, const float *part, float *dbias, hipStream_t st)
 {
     const int L = (2 * g.M - 1) * (2 * g.M - 1);
+    Bias bi{};
+    plan_order(g, dtype, &bi, w.strips);
+    bi.prows = g.M - 1 + most_rows(group_tokens(dtype, g.N), g, bi);
     const int windows = w.shares;
     int runs = 16;
     while (runs > 1 && (runs > windows || (runs / 2 >= windows && w.nblk > 1))) runs /= 2;
-    hipLaunchKernelGGL(reduce_kernel, dim3((L + 63) / 64, g.heads), dim3(1024), 0, st, g, windows, runs, w.nblk, w.prows,
+    hipLaunchKernelGGL(reduce_kernel, dim3((L + 63) / 64, g.heads), dim3(1024), 0, st, g, bi, windows, runs, w.nblk,
                        group_tokens(dtype, g.N), part, dbias);
     return hipGetLastError();
 }

@@ -113,6 +113,8 @@ def test_window_sides(dtype, M):
 def test_head_dims(dtype, d):
     run(dtype, 1, 16, 24, 1 if d % 2 else 2, d, 8, 3, seed=d)
     run(dtype, 1, 18, 9, 1, d, 9, 0, seed=d, packed=True)
+    if d in (7, 15, 30, 47, 64):
+        run(dtype, 1, 16, 16, 1, d, 16, 5, seed=d)
 
 
 @pytest.mark.parametrize("dtype,M,kind", itertools.product(("bf16", "f32"), (4, 7, 16, 18), ("coarse", "near", "past", "none", "one")))
@@ -125,6 +127,7 @@ def test_bucket_maps(dtype, M, kind):
 
 
 @pytest.mark.parametrize("dtype,M,heads,d", [("bf16", 32, 2, 30), ("bf16", 40, 1, 30), ("bf16", 48, 1, 32), ("bf16", 64, 1, 16), ("bf16", 37, 1, 20),
+                                             ("bf16", 32, 1, 15), ("bf16", 48, 1, 33), ("bf16", 96, 1, 8),
                                              ("f32", 32, 1, 30), ("f32", 33, 1, 16), ("f32", 48, 1, 40), ("f32", 64, 1, 16)])
 def test_large_windows(dtype, M, heads, d):
     """Several workgroups a unit; bias rows and sums in chunks of the walk."""
