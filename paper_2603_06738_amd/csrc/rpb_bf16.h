@@ -153,42 +153,49 @@ struct Mover {
         }
     }
 };
-// Columns that no commit writes, once for both stages.  `ones`: in the last two columns of X and Y; `one`: in Y's last column.
+// Columns that no commit writes, once for both stages (beside the first commit: what both write is the same).  `ones`: in the last two
+// columns of X and Y; `ext`: not those columns; `one`: in Y's last column.
 template <int KX, int KY>
-__device__ __forceinline__ void init_cols(const Geo &g, bf16_t *S, bool ones, bool one, int nt)
+__device__ __forceinline__ void init_cols(const Geo &g, bf16_t *S, bool ones, bool ext, bool one, int nt)
 {
     using I = Img<KX, KY>;
     for (int e = threadIdx.x; e < 2 * kTile; e += nt) {
         bf16_t *xr = S + (e / kTile) * I::STAGE + (e % kTile) * I::XS, *yr = S + (e / kTile) * I::STAGE + I::YR + (e % kTile) * I::YS;
-        for (int c = g.d; c < KX; ++c) xr[c] = ones && c >= KX - 2 ? 0x3f80 : 0;
-        for (int c = g.d; c < KY; ++c) yr[c] = (ones && c >= KY - 2) || (one && c == KY - 1) ? 0x3f80 : 0;
+        for (int c = g.d; c < (ext ? KX - 2 : KX); ++c) xr[c] = ones && c >= KX - 2 ? 0x3f80 : 0;
+        for (int c = g.d; c < (ext ? KY - 2 : KY); ++c) yr[c] = (ones && c >= KY - 2) || (one && c == KY - 1) ? 0x3f80 : 0;
     }
 }
 
-// A wave's 64 stationary rows as B operands, through `area` (64 rows of K + 8 columns, the wave's own).
-// f(pass, lane-row, j, raw) may change a piece and gets to write columns of the row.
-template <int K, int LP, int SRC, bool ALN, class Fix>
-__device__ __forceinline__ void stationary_rows(const Geo &g, const Bias &bi, const Win &win, const Rows &s, int n0, bf16_t *area, bf16x8 (&B)[2][K / 16], Fix fix)
-{
-    constexpr int STR = K + 8, R = 64 / LP;             // rows a pass
-    const int lane = threadIdx.x & 63, l = lane / LP, j = lane % LP;
+// A wave's 64 stationary rows of a tensor, LP lanes a row.  Asked for at a workgroup's very start, together with whatever else it needs
+// first, so that it waits for memory once.
+template <int LP>
+struct Held {
     Raw r[LP];
+};
+template <int LP, int SRC, bool ALN>
+__device__ __forceinline__ void hold(Held<LP> &h, const Geo &g, const Bias &bi, const Win &win, const Rows &s, int n0)
+{
+    const int lane = threadIdx.x & 63, l = lane / LP, j = lane % LP;
 #pragma unroll
     for (int p = 0; p < LP; ++p) {
-        const int n = n0 + p * R + l, nc = n < g.N ? n : g.N - 1;
-        const Cell c = cell_of<ALN>(g, bi, nc);
-        r[p] = get_piece<SRC>(s, SRC == kCkpt ? 0u : pixel(win, c), c.index(g), j, g.d);
+        const int n = n0 + p * (64 / LP) + l;
+        const Cell c = cell_of<ALN>(g, bi, n < g.N ? n : g.N - 1);
+        h.r[p] = get_piece<SRC>(s, SRC == kCkpt ? 0u : pixel(win, c), c.index(g), j, g.d);
     }
+}
+// The rows as B operands, through `area` (64 rows of K + 8 columns, the wave's own).  `fix` may change values and writes further columns.
+template <int K, int LP, int SRC, class Fix>
+__device__ __forceinline__ void operands(const Held<LP> &h, const Geo &g, bf16_t *area, bf16x8 (&B)[2][K / 16], Fix fix)
+{
+    constexpr int STR = K + 8;
+    const int lane = threadIdx.x & 63, l = lane / LP, j = lane % LP;
     {
         bf16_t *xr = area + lane * STR;
         for (int c = g.d; c < K; ++c) xr[c] = 0;
     }
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int p = 0; p < LP; ++p) {
-        bf16_t *row = area + (p * R + l) * STR;
-        put_piece<SRC>(row, fix(p, widen_piece<SRC>(r[p])), j, g.d);
-    }
+    for (int p = 0; p < LP; ++p) put_piece<SRC>(area + (p * (64 / LP) + l) * STR, fix(widen_piece<SRC>(h.r[p])), j, g.d);
     __builtin_amdgcn_wave_barrier();
     fix.columns(area, STR);
     __builtin_amdgcn_wave_barrier();
@@ -198,14 +205,14 @@ __device__ __forceinline__ void stationary_rows(const Geo &g, const Bias &bi, co
 }
 struct FixScale {
     float s;            // (1: values as they are)
-    __device__ __forceinline__ Raw operator()(int, const Raw &r) const { return s != 1.f ? scaled(r, s) : r; }
+    __device__ __forceinline__ Raw operator()(const Raw &r) const { return s != 1.f ? scaled(r, s) : r; }
     __device__ __forceinline__ void columns(bf16_t *, int) const {}
 };
 // The pair `w` of row `lane` in the last two columns.
 template <int K>
 struct FixPair {
     uint32_t w;
-    __device__ __forceinline__ Raw operator()(int, const Raw &r) const { return r; }
+    __device__ __forceinline__ Raw operator()(const Raw &r) const { return r; }
     __device__ __forceinline__ void columns(bf16_t *area, int str) const { *(uint32_t *)(area + (threadIdx.x & 63) * str + K - 2) = w; }
 };
 
@@ -310,13 +317,13 @@ constexpr size_t stage_bytes()
 
 // ---- forward -----------------------------------------------------------------------------------------------------
 
-// One walk over the keys.  MAX: with the running maximum of every row.
+// One walk over the keys; `mv` holds the first tile.  MAX: with the running maximum of every row.
 template <bool MAX, int KX, int DB, bool SUM, int SRC, bool ALN, int W>
 __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Place &pl, const Rows &ks, const Rows &vs, bf16_t *S, float *B,
                                          const bf16x8 (&Q)[2][KX / 16], f32x16 (&O)[2][DB], float (&sum)[2], float (&top)[2], const Span &span,
-                                         const int (&mylin)[2], bool active)
+                                         const int (&mylin)[2], bool active, Mover<KX <= 32 ? 4 : 8, W, SRC, SRC, false, ALN> &mv)
 {
-    constexpr int LP = KX <= 32 ? 4 : 8, KY = 32 * DB, NT = 64 * W;
+    constexpr int KY = 32 * DB, NT = 64 * W;
     using I = Img<KX, KY>;
     const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5;
     const int ntiles = (g.N + kTile - 1) / kTile, strip_tiles = ALN ? bi.strip / kTile : ntiles;
@@ -329,8 +336,6 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
             for (int i = 0; i < 16; ++i) O[qb][db][i] = 0.f;
         sum[qb] = 0.f, top[qb] = MAX ? -INFINITY : 0.f;
     }
-    Mover<LP, W, SRC, SRC, false, ALN> mv;
-    mv.request(g, bi, pl.win, ks, vs, nullptr, 0);
     mv.template commit<KX, KY, false>(g, bi, S, 0, 1.f);
     mv.request(g, bi, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
     f32x16 next;            // (ALN) the bias of block (1, the coming one)
@@ -416,7 +421,7 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
 }
 
 template <int KX, int DB, bool SUM, int SRC, bool ALN, int W>
-__global__ __launch_bounds__(W * 64, 2) void fwd_kernel(Geo g, Bias bi, int nblk, int force_max, const bf16_t *__restrict__ q,
+__global__ __launch_bounds__(W * 64, DB == 1 ? 3 : 2) void fwd_kernel(Geo g, Bias bi, int nblk, int force_max, const bf16_t *__restrict__ q,
                                                         const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
                                                         bf16_t *__restrict__ out, float *__restrict__ lse)
 {
@@ -431,8 +436,15 @@ __global__ __launch_bounds__(W * 64, 2) void fwd_kernel(Geo g, Bias bi, int nblk
     const int first = pl.blk * NT, last = first + NT < g.N ? first + NT - 1 : g.N - 1, n0 = first + wave * 64;
     const Span span = span_of<ALN>(g, bi, first, last);
     const bool active = n0 < g.N;
+    const Rows ks = grid_rows(g, pl, k, g.tstride), vs = grid_rows(g, pl, v, g.tstride);
     bf16x8 Q[2][KX / 16];
-    stationary_rows<KX, LP, SRC, ALN>(g, bi, pl.win, grid_rows(g, pl, q, g.tstride), n0, S + wave * 64 * (KX + 8), Q, FixScale{bi.qs});
+    Mover<LP, W, SRC, SRC, false, ALN> mv;
+    {
+        Held<LP> hq;
+        hold<LP, SRC, ALN>(hq, g, bi, pl.win, grid_rows(g, pl, q, g.tstride), n0);
+        mv.request(g, bi, pl.win, ks, vs, nullptr, 0);
+        operands<KX, LP, SRC>(hq, g, S + wave * 64 * (KX + 8), Q, FixScale{bi.qs});
+    }
     int mylin[2];
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
@@ -440,22 +452,23 @@ __global__ __launch_bounds__(W * 64, 2) void fwd_kernel(Geo g, Bias bi, int nblk
         mylin[qb] = cell_of<ALN>(g, bi, n < g.N ? n : g.N - 1).lin(bi);
     }
     __syncthreads();
-    init_cols<KX, 32 * DB>(g, S, false, !SUM, NT);
-    __syncthreads();
-    const Rows ks = grid_rows(g, pl, k, g.tstride), vs = grid_rows(g, pl, v, g.tstride);
+    init_cols<KX, 32 * DB>(g, S, false, false, !SUM, NT);
     f32x16 O[2][DB];
     float sum[2], top[2];
     // First without a running maximum: exp2 of a logit is a normal number far beyond what bounded logits need.  A row whose
     // denominator leaves [2^-60, 2^60], and not for want of keys, sends the workgroup on a second walk, with one.
     bool bad = true;
     if (!force_max) {
-        fwd_walk<false, KX, DB, SUM, SRC, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, mylin, active);
+        fwd_walk<false, KX, DB, SUM, SRC, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, mylin, active, mv);
         bad = false;
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb)
             if (active && bad_rows(g, bi, pl.hd, n0 + qb * 32 + col < g.N ? cell_of<ALN>(g, bi, n0 + qb * 32 + col).index(g) : g.N, sum[qb])) bad = true;
     }
-    if (__syncthreads_or(bad)) fwd_walk<true, KX, DB, SUM, SRC, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, mylin, active);
+    if (__syncthreads_or(bad)) {
+        mv.request(g, bi, pl.win, ks, vs, nullptr, 0);
+        fwd_walk<true, KX, DB, SUM, SRC, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, mylin, active, mv);
+    }
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
         const int n = n0 + qb * 32 + col;
@@ -494,46 +507,45 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
     __syncthreads();
     const int first = pl.blk * NT, last = first + NT < g.N ? first + NT - 1 : g.N - 1, n0 = first + wave * 64;
     const Span span = span_of<ALN>(g, bi, first, last);
+    const Span own = span_of<ALN>(g, bi, n0 < g.N ? n0 : g.N - 1, n0 + 63 < g.N ? n0 + 63 : g.N - 1);      // the wave's own rows
     const bool active = n0 < g.N;
+    const Rows ks = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 1) : grid_rows(g, pl, k, g.tstride);
+    const Rows vs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 2) : grid_rows(g, pl, v, g.tstride);
     bf16x8 Q[2][K / 16], D[2][K / 16];
+    Mover<LP, W, SRC, SRC, false, ALN> mv;
     float L;            // LSE in base 2 of row `lane`
     {
+        Held<LP> hq, hd, ho;
+        hold<LP, SG, ALN>(hd, g, bi, pl.win, grid_rows(g, pl, dout, g.C), n0);
+        hold<LP, SG, ALN>(ho, g, bi, pl.win, grid_rows(g, pl, out, g.C), n0);
+        const int n = n0 + lane, nc = n < g.N ? n : g.N - 1;
+        const float e = lse[(int64_t)pl.u * g.N + cell_of<ALN>(g, bi, nc).index(g)];
+        hold<LP, SRC, ALN>(hq, g, bi, pl.win, SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 0) : grid_rows(g, pl, q, g.tstride), n0);
+        mv.request(g, bi, pl.win, ks, vs, nullptr, 0);
         // delta of the wave's rows: LP lanes share one
-        const Rows os = grid_rows(g, pl, out, g.C), ds = grid_rows(g, pl, dout, g.C);
-        const int l = lane / LP, j = lane % LP, c = piece_col<SG>(j, g.d);
-        float dl[LP];
+        const int j = lane % LP, c = piece_col<SG>(j, g.d);
+        float delta = 0.f;      // of row `lane`: it belongs to pass lane / (64 / LP), lanes (lane % (64 / LP)) * LP ..
 #pragma unroll
         for (int p = 0; p < LP; ++p) {
-            const int n = n0 + p * (64 / LP) + l, nc = n < g.N ? n : g.N - 1;
-            const uint32_t t = pixel(pl.win, cell_of<ALN>(g, bi, nc));
-            const Raw a = get_piece<SG>(os, t, 0, j, g.d), b = get_piece<SG>(ds, t, 0, j, g.d);
             float s = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {       // (a piece that slid back holds a neighbour's values first)
-                const float x = e & 1 ? hi_bf16(a.w[e >> 1]) * hi_bf16(b.w[e >> 1]) : lo_bf16(a.w[e >> 1]) * lo_bf16(b.w[e >> 1]);
-                s += SG == kAny || c + e >= 8 * j ? x : 0.f;
+            for (int i = 0; i < 8; ++i) {       // (a piece that slid back holds a neighbour's values first)
+                const uint32_t a = ho.r[p].w[i >> 1], b = hd.r[p].w[i >> 1];
+                const float x = i & 1 ? hi_bf16(a) * hi_bf16(b) : lo_bf16(a) * lo_bf16(b);
+                s += SG == kAny || c + i >= 8 * j ? x : 0.f;
             }
 #pragma unroll
             for (int m = 1; m < LP; m <<= 1) s += __shfl_xor(s, m);
-            dl[p] = s;
-        }
-        // row `lane` belongs to pass lane / (64 / LP), lanes (lane % (64 / LP)) * LP ..
-        float delta = 0.f;
-#pragma unroll
-        for (int p = 0; p < LP; ++p) {
-            const float x = __shfl(dl[p], (lane % (64 / LP)) * LP);
+            const float x = __shfl(s, (lane % (64 / LP)) * LP);
             if (lane / (64 / LP) == p) delta = x;
         }
-        const int n = n0 + lane, nc = n < g.N ? n : g.N - 1;
-        const float e = lse[(int64_t)pl.u * g.N + cell_of<ALN>(g, bi, nc).index(g)];
         const bool none = n >= g.N || e == -INFINITY;
         const uint32_t wl = none ? pack_bf16(-kNoRow, 0.f) : split_bf16(-e * bi.bs), wd = split_bf16(-delta);
         L = none ? kNoRow : e * kLog2e;
         if (n < g.N) ext[(int64_t)pl.u * g.N + n] = uint2{wl, wd};
         bf16_t *area = S + wave * 64 * (K + 8);
-        const Rows qs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 0) : grid_rows(g, pl, q, g.tstride);
-        stationary_rows<K, LP, SRC, ALN>(g, bi, pl.win, qs, n0, area, Q, FixScale{bi.qs});
-        stationary_rows<K, LP, SG, ALN>(g, bi, pl.win, ds, n0, area, D, FixPair<K>{wd});
+        operands<K, LP, SRC>(hq, g, area, Q, FixScale{bi.qs});
+        operands<K, LP, SG>(hd, g, area, D, FixPair<K>{wd});
     }
     int mylin[2];
     float mylse[2];
@@ -543,13 +555,8 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
         mylin[qb] = cell_of<ALN>(g, bi, n < g.N ? n : g.N - 1).lin(bi);
         mylse[qb] = __shfl(L, qb * 32 + col);
     }
-    // (the wave's own last window row, for its histogram)
-    const int wsy1 = span_of<ALN>(g, bi, n0 < g.N ? n0 : g.N - 1, n0 + 63 < g.N ? n0 + 63 : g.N - 1).y1;
     __syncthreads();
-    init_cols<K, K>(g, S, true, false, NT);
-    __syncthreads();
-    const Rows ks = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 1) : grid_rows(g, pl, k, g.tstride);
-    const Rows vs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 2) : grid_rows(g, pl, v, g.tstride);
+    init_cols<K, K>(g, S, true, false, false, NT);
     f32x16 A[2][DB];
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb)
@@ -560,8 +567,6 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
     const int ntiles = (g.N + kTile - 1) / kTile, strip_tiles = ALN ? bi.strip / kTile : ntiles;
     const int tro = tr_lane_offset<I::XS>(lane), ako = col * I::XS + 8 * hf;
     const f32x16 z = {0};
-    Mover<LP, W, SRC, SRC, false, ALN> mv;
-    mv.request(g, bi, pl.win, ks, vs, nullptr, 0);
     mv.template commit<K, K, true>(g, bi, S, 0, 1.f);
     mv.request(g, bi, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
     f32x16 next, held;      // (ALN) the bias of block (1, the coming one); dS of block (0, the last one)
@@ -571,7 +576,7 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
         t1 = t0 + bi.chunk < end ? t0 + bi.chunk : end;
         const Chunk ch = chunk_of<ALN>(g, bi, t0, t1, span);
         stage_bias<-1>(g, bi, ch, pl.hd, bi.bs, B, NT);
-        double *const mine = H + wave * hsize + ch.c0 - (span.y1 - wsy1) * bi.ws;
+        double *const mine = H + wave * hsize + ch.c0 - (span.y1 - own.y1) * bi.ws;
         __syncthreads();
         if (ALN && t0 * kTile == ch.t0 && active) next = bias_block<ALN>(B + ch.c0 - mylin[1], words_of<ALN>(bi, ch, nullptr, t0, 0, hf));
         for (int tile = t0; tile < t1; ++tile) {
@@ -663,13 +668,18 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
     const int first = pl.blk * NT, last = first + NT < g.N ? first + NT - 1 : g.N - 1, n0 = first + wave * 64;
     const Span span = span_of<ALN>(g, bi, first, last);
     const bool active = n0 < g.N;
+    const Rows qs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 0) : grid_rows(g, pl, q, g.tstride), ds = grid_rows(g, pl, dout, g.C);
+    const uint2 *const ex = ext + (int64_t)pl.u * g.N;
     bf16x8 Kb[2][K / 16], Vb[2][K / 16];
+    Mover<LP, W, SRC, SG, true, ALN> mv;
     {
+        Held<LP> hk, hv;
+        hold<LP, SRC, ALN>(hk, g, bi, pl.win, SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 1) : grid_rows(g, pl, k, g.tstride), n0);
+        hold<LP, SRC, ALN>(hv, g, bi, pl.win, SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 2) : grid_rows(g, pl, v, g.tstride), n0);
+        mv.request(g, bi, pl.win, qs, ds, ex, 0);
         bf16_t *area = S + wave * 64 * (K + 8);
-        const Rows ks = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 1) : grid_rows(g, pl, k, g.tstride);
-        const Rows vs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 2) : grid_rows(g, pl, v, g.tstride);
-        stationary_rows<K, LP, SRC, ALN>(g, bi, pl.win, ks, n0, area, Kb, FixPair<K>{kOnes});
-        stationary_rows<K, LP, SRC, ALN>(g, bi, pl.win, vs, n0, area, Vb, FixPair<K>{kOnes});
+        operands<K, LP, SRC>(hk, g, area, Kb, FixPair<K>{kOnes});
+        operands<K, LP, SRC>(hv, g, area, Vb, FixPair<K>{kOnes});
     }
     int mylin[2];
 #pragma unroll
@@ -678,10 +688,7 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
         mylin[b] = cell_of<ALN>(g, bi, n < g.N ? n : g.N - 1).lin(bi);
     }
     __syncthreads();
-    init_cols<K, K>(g, S, false, false, NT);
-    __syncthreads();
-    const Rows qs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 0) : grid_rows(g, pl, q, g.tstride), ds = grid_rows(g, pl, dout, g.C);
-    const uint2 *const ex = ext + (int64_t)pl.u * g.N;
+    init_cols<K, K>(g, S, false, true, false, NT);
     f32x16 Ak[2][DB], Av[2][DB];
 #pragma unroll
     for (int b = 0; b < 2; ++b)
@@ -694,8 +701,6 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
     const float scale = bi.qs;
     const f32x16 z = {0};
     f32x16 next;            // (ALN) the bias of block (1, the coming one)
-    Mover<LP, W, SRC, SG, true, ALN> mv;
-    mv.request(g, bi, pl.win, qs, ds, ex, 0);
     mv.template commit<K, K, false>(g, bi, S, 0, scale);
     mv.request(g, bi, pl.win, qs, ds, ex, ntiles > 1 ? 1 : 0);
     for (int t0 = 0, t1, end = strip_tiles; t0 < ntiles; t0 = t1) {

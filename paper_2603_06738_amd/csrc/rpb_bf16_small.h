@@ -54,11 +54,7 @@ __device__ __forceinline__ Rows rows_at(const Geo &g, const Spot &s, int hd, con
     return Rows{(const char *)x + (s.img * stride + hd * g.d) * 2, stride * 2, nullptr};
 }
 
-// 64 rows of a tensor, LP lanes a row.
-template <int LP>
-struct Held {
-    Raw r[LP];
-};
+// A window's rows of a tensor, by their pixels `t`.
 template <int LP, int SRC>
 __device__ __forceinline__ void hold(Held<LP> &h, const Geo &g, const Rows &s, const uint32_t (&t)[LP])
 {
