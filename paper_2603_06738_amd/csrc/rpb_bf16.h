@@ -2,7 +2,8 @@
 // the bias's gradient, then dkv).  Operator: include/rib_attn.h; the walk and the bias in LDS: rpb_common.h.
 //
 // A wave owns 64 stationary tokens as MFMA B operands, a workgroup W waves; the other side of the unit streams through LDS in
-// tiles of 64 token rows, two stages in turn.  Scores are 32x32 blocks with the streamed tokens as rows, so a lane owns one
+// tiles of 64 token rows, two stages in turn.  (SPLIT, for grids that would leave most of the chip idle: four waves share 64 stationary
+// tokens, two blocks of them by two of every tile's; the sums of a block's two waves are added through LDS at the end.)  Scores are 32x32 blocks with the streamed tokens as rows, so a lane owns one
 // stationary token and 16 streamed ones; their bias is the C operand of the score product.  What is packed to bf16 there
 // (P, dS) is the B operand of the product that contracts over the streamed tokens, whose A operand is read transposed from
 // the same rows.  Products of q and k are exact in fp32 and scaled there: rounding a scaled q to bf16 would save 16 of some 100 vector
@@ -183,9 +184,9 @@ __device__ __forceinline__ void hold(Held<LP> &h, const Geo &g, const Bias &bi, 
         h.r[p] = get_piece<SRC>(s, SRC == kCkpt ? 0u : pixel(win, c), c.index(g), j, g.d);
     }
 }
-// The rows as B operands, through `area` (64 rows of K + 8 columns, the wave's own).  `fix` may change values and writes further columns.
-template <int K, int LP, int SRC, class Fix>
-__device__ __forceinline__ void operands(const Held<LP> &h, const Geo &g, bf16_t *area, bf16x8 (&B)[2][K / 16], Fix fix)
+// QB blocks of the rows, from block `sel` on, as B operands, through `area` (64 rows of K + 8 columns, the wave's own).  `fix` may change values and writes further columns.
+template <int K, int LP, int SRC, int QB, class Fix>
+__device__ __forceinline__ void operands(const Held<LP> &h, const Geo &g, bf16_t *area, bf16x8 (&B)[QB][K / 16], int sel, Fix fix)
 {
     constexpr int STR = K + 8;
     const int lane = threadIdx.x & 63, l = lane / LP, j = lane % LP;
@@ -200,7 +201,7 @@ __device__ __forceinline__ void operands(const Held<LP> &h, const Geo &g, bf16_t
     fix.columns(area, STR);
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int b = 0; b < 2; ++b) read_rows<K / 16>(B[b], area + (b * 32 + (lane & 31)) * STR + 8 * (lane >> 5));
+    for (int b = 0; b < QB; ++b) read_rows<K / 16>(B[b], area + ((sel + b) * 32 + (lane & 31)) * STR + 8 * (lane >> 5));
     __builtin_amdgcn_wave_barrier();
 }
 struct FixScale {
@@ -315,21 +316,41 @@ constexpr size_t stage_bytes()
     return ((tiles > stat ? tiles : stat) + 15) & ~(size_t)15;
 }
 
+// Adds the odd waves' sums to their even neighbours', through `lds` (16 * 64 floats a block and pair of waves).
+template <int DB>
+__device__ __forceinline__ void join(f32x16 (&v)[DB], float *lds, bool odd)
+{
+    float *const part = lds + (threadIdx.x >> 7) * DB * 16 * 64 + (threadIdx.x & 63);
+    __syncthreads();
+    if (odd)
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) part[(16 * db + i) * 64] = v[db][i];
+    __syncthreads();
+    if (!odd)
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[db][i] += part[(16 * db + i) * 64];
+}
+
 // ---- forward -----------------------------------------------------------------------------------------------------
 
 // One walk over the keys; `mv` holds the first tile.  MAX: with the running maximum of every row.
-template <bool MAX, int KX, int DB, bool SUM, int SRC, bool ALN, int W>
+template <bool MAX, int KX, int DB, bool SUM, int SRC, bool ALN, bool SPLIT, int W>
 __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Place &pl, const Rows &ks, const Rows &vs, bf16_t *S, float *B,
-                                         const bf16x8 (&Q)[2][KX / 16], f32x16 (&O)[2][DB], float (&sum)[2], float (&top)[2], const Span &span,
-                                         const int (&mylin)[2], bool active, Mover<KX <= 32 ? 4 : 8, W, SRC, SRC, false, ALN> &mv)
+                                         const bf16x8 (&Q)[SPLIT ? 1 : 2][KX / 16], f32x16 (&O)[SPLIT ? 1 : 2][DB], float (&sum)[SPLIT ? 1 : 2], float (&top)[SPLIT ? 1 : 2], const Span &span,
+                                         const int (&mylin)[SPLIT ? 1 : 2], bool active, Mover<KX <= 32 ? 4 : 8, W, SRC, SRC, false, ALN> &mv)
 {
-    constexpr int KY = 32 * DB, NT = 64 * W;
+    constexpr int KY = 32 * DB, NT = 64 * W, QB = SPLIT ? 1 : 2;
+    constexpr bool CARRY = ALN && !SPLIT;
     using I = Img<KX, KY>;
-    const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5;
+    const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5, half = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 1;
     const int ntiles = (g.N + kTile - 1) / kTile, strip_tiles = ALN ? bi.strip / kTile : ntiles;
     const int tro = tr_lane_offset<I::YS>(lane), ako = col * I::XS + 8 * hf;
 #pragma unroll
-    for (int qb = 0; qb < 2; ++qb) {
+    for (int qb = 0; qb < QB; ++qb) {
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -338,13 +359,13 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
     }
     mv.template commit<KX, KY, false>(g, bi, S, 0, 1.f);
     mv.request(g, bi, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
-    f32x16 next;            // (ALN) the bias of block (1, the coming one)
+    f32x16 next;            // (CARRY) the bias of block (1, the coming one)
     for (int t0 = 0, t1, end = strip_tiles; t0 < ntiles; t0 = t1) {
         t1 = t0 + bi.chunk < end ? t0 + bi.chunk : end;
         const Chunk ch = chunk_of<ALN>(g, bi, t0, t1, span);
         stage_bias<-1>(g, bi, ch, pl.hd, bi.bs, B, NT);
         __syncthreads();
-        if (ALN && t0 * kTile == ch.t0 && active) next = bias_block<ALN>(B + ch.c0 - mylin[1], words_of<ALN>(bi, ch, nullptr, t0, 0, hf));
+        if (CARRY && t0 * kTile == ch.t0 && active) next = bias_block<ALN>(B + ch.c0 - mylin[QB - 1], words_of<ALN>(bi, ch, nullptr, t0, 0, hf));
         for (int tile = t0; tile < t1; ++tile) {
             const bf16_t *cur = S + (tile & 1) * I::STAGE;
             if (tile + 1 < ntiles) {
@@ -353,8 +374,8 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
             }
             if (active) {
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    const int key0 = tile * kTile + kb * 32;
+                for (int kx = 0; kx < (SPLIT ? 1 : 2); ++kx) {
+                    const int kb = SPLIT ? half : kx, key0 = tile * kTile + kb * 32;
                     if (!ALN && key0 >= g.N) break;
                     const Words16<ALN> wd = words_of<ALN>(bi, ch, (const int *)(cur + I::LT), tile, kb, hf);
                     bf16x8 Ak[KX / 16], At[DB][2];
@@ -364,10 +385,10 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
 #pragma unroll
                         for (int i = 0; i < 2; ++i) At[db][i] = read_tr<I::YS>(cur + I::YR + (kb * 32 + 16 * i) * I::YS, tro, 32 * db);
 #pragma unroll
-                    for (int qx = 0; qx < 2; ++qx) {
-                        const int qb = 1 - qx;
-                        f32x16 s = ALN && qb == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[qb], wd);
-                        if (ALN && qb == 0) next = s;
+                    for (int qx = 0; qx < QB; ++qx) {
+                        const int qb = QB - 1 - qx;
+                        f32x16 s = CARRY && qb == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[qb], wd);
+                        if (CARRY && qb == 0) next = s;
 #pragma unroll
                         for (int i = 0; i < KX / 16; ++i) s = mfma(Ak[i], Q[qb][i], s);
                         if (!ALN) mask_rows(s, key0, g.N, hf);
@@ -412,20 +433,46 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
         }
         if (t1 == end) end += strip_tiles;
     }
+    if constexpr (SPLIT) {
+        // the two halves' sums; with maxima of their own they are first brought to the larger one
+        float *const part = (float *)S + (threadIdx.x >> 7) * (16 * DB + 2) * 64 + lane;
+        if (half) {
+            part[0] = top[0], part[64] = sum[0];
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) part[(2 + 16 * db + i) * 64] = O[0][db][i];
+        }
+        __syncthreads();
+        if (!half) {
+            float a = 1.f, b = 1.f;
+            if (MAX) {
+                const float m = fmaxf(top[0], part[0]), ms = m == -INFINITY ? 0.f : m;
+                a = __builtin_amdgcn_exp2f(top[0] - ms), b = __builtin_amdgcn_exp2f(part[0] - ms);
+                top[0] = m;
+            }
+            sum[0] = sum[0] * a + part[64] * b;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) O[0][db][i] = O[0][db][i] * a + part[(2 + 16 * db + i) * 64] * b;
+        }
+        __syncthreads();
+    }
     // the denominator: the last row of O^T is register 15 of the upper lane half
 #pragma unroll
-    for (int qb = 0; qb < 2; ++qb) {
+    for (int qb = 0; qb < QB; ++qb) {
         const float mine = SUM ? sum[qb] : O[qb][DB - 1][15], other = __shfl_xor(mine, 32);
         sum[qb] = SUM ? mine + other : hf ? mine : other;
     }
 }
 
-template <int KX, int DB, bool SUM, int SRC, bool ALN, int W>
+template <int KX, int DB, bool SUM, int SRC, bool ALN, bool SPLIT, int W>
 __global__ __launch_bounds__(W * 64, DB == 1 ? 3 : 2) void fwd_kernel(Geo g, Bias bi, int nblk, int force_max, const bf16_t *__restrict__ q,
                                                         const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
                                                         bf16_t *__restrict__ out, float *__restrict__ lse)
 {
-    constexpr int LP = KX <= 32 ? 4 : 8, NT = 64 * W;
+    constexpr int LP = KX <= 32 ? 4 : 8, NT = 64 * W, QB = SPLIT ? 1 : 2, GT = SPLIT ? 64 : NT;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     bf16_t *S = (bf16_t *)smem;
     int *map = (int *)(smem + stage_bytes<KX, 32 * DB, W>());
@@ -433,45 +480,47 @@ __global__ __launch_bounds__(W * 64, DB == 1 ? 3 : 2) void fwd_kernel(Geo g, Bia
     const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place pl = place_of(g, nblk, NT, map);
     __syncthreads();
-    const int first = pl.blk * NT, last = first + NT < g.N ? first + NT - 1 : g.N - 1, n0 = first + wave * 64;
+    const int first = pl.blk * GT, last = first + GT < g.N ? first + GT - 1 : g.N - 1, n0 = first + (SPLIT ? 0 : wave * 64), sel = SPLIT ? wave >> 1 : 0, half = wave & 1;
     const Span span = span_of<ALN>(g, bi, first, last);
     const bool active = n0 < g.N;
     const Rows ks = grid_rows(g, pl, k, g.tstride), vs = grid_rows(g, pl, v, g.tstride);
-    bf16x8 Q[2][KX / 16];
+    bf16x8 Q[QB][KX / 16];
     Mover<LP, W, SRC, SRC, false, ALN> mv;
     {
         Held<LP> hq;
         hold<LP, SRC, ALN>(hq, g, bi, pl.win, grid_rows(g, pl, q, g.tstride), n0);
         mv.request(g, bi, pl.win, ks, vs, nullptr, 0);
-        operands<KX, LP, SRC>(hq, g, S + wave * 64 * (KX + 8), Q, FixScale{bi.qs});
+        operands<KX, LP, SRC, QB>(hq, g, S + wave * 64 * (KX + 8), Q, sel, FixScale{bi.qs});
     }
-    int mylin[2];
+    int mylin[QB];
 #pragma unroll
-    for (int qb = 0; qb < 2; ++qb) {
-        const int n = n0 + qb * 32 + col;
+    for (int qb = 0; qb < QB; ++qb) {
+        const int n = n0 + (sel + qb) * 32 + col;
         mylin[qb] = cell_of<ALN>(g, bi, n < g.N ? n : g.N - 1).lin(bi);
     }
     __syncthreads();
     init_cols<KX, 32 * DB>(g, S, false, false, !SUM, NT);
-    f32x16 O[2][DB];
-    float sum[2], top[2];
+    f32x16 O[QB][DB];
+    float sum[QB], top[QB];
     // First without a running maximum: exp2 of a logit is a normal number far beyond what bounded logits need.  A row whose
     // denominator leaves [2^-60, 2^60], and not for want of keys, sends the workgroup on a second walk, with one.
     bool bad = true;
     if (!force_max) {
-        fwd_walk<false, KX, DB, SUM, SRC, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, mylin, active, mv);
+        fwd_walk<false, KX, DB, SUM, SRC, ALN, SPLIT, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, mylin, active, mv);
         bad = false;
 #pragma unroll
-        for (int qb = 0; qb < 2; ++qb)
-            if (active && bad_rows(g, bi, pl.hd, n0 + qb * 32 + col < g.N ? cell_of<ALN>(g, bi, n0 + qb * 32 + col).index(g) : g.N, sum[qb])) bad = true;
+        for (int qb = 0; qb < QB; ++qb)
+            if (active && !(SPLIT && half) && bad_rows(g, bi, pl.hd, n0 + (sel + qb) * 32 + col < g.N ? cell_of<ALN>(g, bi, n0 + (sel + qb) * 32 + col).index(g) : g.N, sum[qb])) bad = true;
     }
     if (__syncthreads_or(bad)) {
         mv.request(g, bi, pl.win, ks, vs, nullptr, 0);
-        fwd_walk<true, KX, DB, SUM, SRC, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, mylin, active, mv);
+        if (SPLIT) init_cols<KX, 32 * DB>(g, S, false, false, !SUM, NT);       // (the first walk's sums went through the tiles)
+        fwd_walk<true, KX, DB, SUM, SRC, ALN, SPLIT, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, mylin, active, mv);
     }
+    if (SPLIT && half) return;
 #pragma unroll
-    for (int qb = 0; qb < 2; ++qb) {
-        const int n = n0 + qb * 32 + col;
+    for (int qb = 0; qb < QB; ++qb) {
+        const int n = n0 + (sel + qb) * 32 + col;
         if (n >= g.N) continue;
         const Cell c = cell_of<ALN>(g, bi, n);
         const float inv = sum[qb] == 0.f ? 0.f : 1.f / sum[qb];         // (a row without a key: zeros)
@@ -485,14 +534,15 @@ __global__ __launch_bounds__(W * 64, DB == 1 ? 3 : 2) void fwd_kernel(Geo g, Bia
 
 // ---- backward: dq and the bias's gradient -------------------------------------------------------------------------
 
-template <int K, int DB, int SRC, int SG, bool ALN, int W, bool HIST>
+template <int K, int DB, int SRC, int SG, bool ALN, bool SPLIT, int W, bool HIST>
 __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk, const bf16_t *__restrict__ q,
                                                        const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
                                                        const uint8_t *__restrict__ ckpt, const bf16_t *__restrict__ out,
                                                        const bf16_t *__restrict__ dout, const float *__restrict__ lse,
                                                        bf16_t *__restrict__ dq, uint2 *__restrict__ ext, float *__restrict__ part)
 {
-    constexpr int LP = DB == 1 ? 4 : 8, NT = 64 * W;
+    constexpr int LP = DB == 1 ? 4 : 8, NT = 64 * W, QB = SPLIT ? 1 : 2, GT = SPLIT ? 64 : NT;      // (GT: the workgroup's stationary tokens)
+    constexpr bool CARRY = ALN && !SPLIT;
     using I = Img<K, K>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     bf16_t *S = (bf16_t *)smem;
@@ -505,13 +555,13 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
     if (HIST)
         for (int e = threadIdx.x; e < W * hsize; e += NT) H[e] = 0.;
     __syncthreads();
-    const int first = pl.blk * NT, last = first + NT < g.N ? first + NT - 1 : g.N - 1, n0 = first + wave * 64;
+    const int first = pl.blk * GT, last = first + GT < g.N ? first + GT - 1 : g.N - 1, n0 = first + (SPLIT ? 0 : wave * 64), sel = SPLIT ? wave >> 1 : 0, half = wave & 1;
     const Span span = span_of<ALN>(g, bi, first, last);
     const Span own = span_of<ALN>(g, bi, n0 < g.N ? n0 : g.N - 1, n0 + 63 < g.N ? n0 + 63 : g.N - 1);      // the wave's own rows
     const bool active = n0 < g.N;
     const Rows ks = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 1) : grid_rows(g, pl, k, g.tstride);
     const Rows vs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 2) : grid_rows(g, pl, v, g.tstride);
-    bf16x8 Q[2][K / 16], D[2][K / 16];
+    bf16x8 Q[QB][K / 16], D[QB][K / 16];
     Mover<LP, W, SRC, SRC, false, ALN> mv;
     float L;            // LSE in base 2 of row `lane`
     {
@@ -544,22 +594,22 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
         L = none ? kNoRow : e * kLog2e;
         if (n < g.N) ext[(int64_t)pl.u * g.N + n] = uint2{wl, wd};
         bf16_t *area = S + wave * 64 * (K + 8);
-        operands<K, LP, SRC>(hq, g, area, Q, FixScale{bi.qs});
-        operands<K, LP, SG>(hd, g, area, D, FixPair<K>{wd});
+        operands<K, LP, SRC, QB>(hq, g, area, Q, sel, FixScale{bi.qs});
+        operands<K, LP, SG, QB>(hd, g, area, D, sel, FixPair<K>{wd});
     }
-    int mylin[2];
-    float mylse[2];
+    int mylin[QB];
+    float mylse[QB];
 #pragma unroll
-    for (int qb = 0; qb < 2; ++qb) {
-        const int n = n0 + qb * 32 + col;
+    for (int qb = 0; qb < QB; ++qb) {
+        const int n = n0 + (sel + qb) * 32 + col;
         mylin[qb] = cell_of<ALN>(g, bi, n < g.N ? n : g.N - 1).lin(bi);
-        mylse[qb] = __shfl(L, qb * 32 + col);
+        mylse[qb] = __shfl(L, (sel + qb) * 32 + col);
     }
     __syncthreads();
     init_cols<K, K>(g, S, true, false, false, NT);
-    f32x16 A[2][DB];
+    f32x16 A[QB][DB];
 #pragma unroll
-    for (int qb = 0; qb < 2; ++qb)
+    for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -569,8 +619,8 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
     const f32x16 z = {0};
     mv.template commit<K, K, true>(g, bi, S, 0, 1.f);
     mv.request(g, bi, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
-    f32x16 next, held;      // (ALN) the bias of block (1, the coming one); dS of block (0, the last one)
-    if (ALN && HIST) held = z;
+    f32x16 next, held;      // (CARRY) the bias of block (1, the coming one); dS of block (0, the last one)
+    if (CARRY && HIST) held = z;
     int before = -1;            // last streamed row of the strip's chunk before
     for (int t0 = 0, t1, end = strip_tiles; t0 < ntiles; t0 = t1) {
         t1 = t0 + bi.chunk < end ? t0 + bi.chunk : end;
@@ -578,7 +628,7 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
         stage_bias<-1>(g, bi, ch, pl.hd, bi.bs, B, NT);
         double *const mine = H + wave * hsize + ch.c0 - (span.y1 - own.y1) * bi.ws;
         __syncthreads();
-        if (ALN && t0 * kTile == ch.t0 && active) next = bias_block<ALN>(B + ch.c0 - mylin[1], words_of<ALN>(bi, ch, nullptr, t0, 0, hf));
+        if (CARRY && t0 * kTile == ch.t0 && active) next = bias_block<ALN>(B + ch.c0 - mylin[QB - 1], words_of<ALN>(bi, ch, nullptr, t0, 0, hf));
         for (int tile = t0; tile < t1; ++tile) {
             const bf16_t *cur = S + (tile & 1) * I::STAGE;
             if (tile + 1 < ntiles) {
@@ -587,8 +637,8 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
             }
             if (active) {
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    const int key0 = tile * kTile + kb * 32;
+                for (int kx = 0; kx < (SPLIT ? 1 : 2); ++kx) {
+                    const int kb = SPLIT ? half : kx, key0 = tile * kTile + kb * 32;
                     if (!ALN && key0 >= g.N) break;
                     const Words16<ALN> wd = words_of<ALN>(bi, ch, (const int *)(cur + I::LT), tile, kb, hf);
                     bf16x8 Ak[K / 16], Av[K / 16], At[DB][2];
@@ -599,10 +649,10 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
 #pragma unroll
                         for (int i = 0; i < 2; ++i) At[db][i] = read_tr<I::XS>(cur + (kb * 32 + 16 * i) * I::XS, tro, 32 * db);
 #pragma unroll
-                    for (int qx = 0; qx < 2; ++qx) {
-                        const int qb = 1 - qx;
-                        f32x16 s = ALN && qb == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[qb], wd), p = z;
-                        if (ALN && qb == 0) next = s;
+                    for (int qx = 0; qx < QB; ++qx) {
+                        const int qb = QB - 1 - qx;
+                        f32x16 s = CARRY && qb == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[qb], wd), p = z;
+                        if (CARRY && qb == 0) next = s;
 #pragma unroll
                         for (int i = 0; i < K / 16; ++i) s = mfma(Ak[i], Q[qb][i], s);
 #pragma unroll
@@ -610,9 +660,9 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
                         if (!ALN) mask_rows(s, key0, g.N, hf);
 #pragma unroll
                         for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], bi.c, -mylse[qb])) * p[i];
-                        if (HIST && ALN && qb == 1) add_offsets<ALN>(mine - mylin[1], wd, s + held);
-                        else if (HIST && ALN) held = s;
-                        else if (HIST && (ALN || n0 + qb * 32 + col < g.N)) add_offsets<ALN>(mine - mylin[qb], wd, s);     // (many lanes at one word are slow)
+                        if (HIST && CARRY && qb == 1) add_offsets<ALN>(mine - mylin[QB - 1], wd, s + held);
+                        else if (HIST && CARRY) held = s;
+                        else if (HIST && (ALN || n0 + (sel + qb) * 32 + col < g.N)) add_offsets<ALN>(mine - mylin[qb], wd, s);     // (many lanes at one word are slow)
                         uint32_t P[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) P[i] = pack_bf16(s[2 * i], s[2 * i + 1]);
@@ -627,20 +677,24 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
             __syncthreads();
         }
         if (HIST) {
-            if (ALN && t1 == end) {
+            if (CARRY && t1 == end) {
                 if (active) add_offsets<ALN>(mine - mylin[0], words_of<ALN>(bi, ch, nullptr, t1 - 1, 1, hf), held);
                 held = z;
                 __syncthreads();
             }
-            flush<ALN, W, 64>(g, bi, ch, H, hsize, first, before,
+            flush<ALN, W, SPLIT ? 0 : 64, 64>(g, bi, ch, H, hsize, first, before,
                               part + sums_at(g, bi, pl.u, nblk, pl.blk, bi.prows, ch.t.x0) + ch.t.y0 * bi.ws);
             before = t1 == end ? -1 : ch.t.y1;
         }
         if (t1 == end) end += strip_tiles;
     }
+    if constexpr (SPLIT) {
+        join<DB>(A[0], (float *)S, half);
+        if (half) return;
+    }
 #pragma unroll
-    for (int qb = 0; qb < 2; ++qb) {
-        const int n = n0 + qb * 32 + col;
+    for (int qb = 0; qb < QB; ++qb) {
+        const int n = n0 + (sel + qb) * 32 + col;
         if (n >= g.N) continue;
         bf16_t *row = dq + (pl.img + pixel(pl.win, cell_of<ALN>(g, bi, n))) * g.C + pl.hd * g.d;
 #pragma unroll
@@ -650,13 +704,14 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
 
 // ---- backward: dk, dv --------------------------------------------------------------------------------------------
 
-template <int K, int DB, int SRC, int SG, bool ALN, int W>
+template <int K, int DB, int SRC, int SG, bool ALN, bool SPLIT, int W>
 __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk, const bf16_t *__restrict__ q,
                                                         const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
                                                         const uint8_t *__restrict__ ckpt, const bf16_t *__restrict__ dout,
                                                         const uint2 *__restrict__ ext, bf16_t *__restrict__ dk, bf16_t *__restrict__ dv)
 {
-    constexpr int LP = DB == 1 ? 4 : 8, NT = 64 * W;
+    constexpr int LP = DB == 1 ? 4 : 8, NT = 64 * W, QB = SPLIT ? 1 : 2, GT = SPLIT ? 64 : NT;      // (GT: the workgroup's stationary tokens)
+    constexpr bool CARRY = ALN && !SPLIT;
     using I = Img<K, K>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     bf16_t *S = (bf16_t *)smem;
@@ -665,12 +720,12 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
     const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place pl = place_of(g, nblk, NT, map);
     __syncthreads();
-    const int first = pl.blk * NT, last = first + NT < g.N ? first + NT - 1 : g.N - 1, n0 = first + wave * 64;
+    const int first = pl.blk * GT, last = first + GT < g.N ? first + GT - 1 : g.N - 1, n0 = first + (SPLIT ? 0 : wave * 64), sel = SPLIT ? wave >> 1 : 0, half = wave & 1;
     const Span span = span_of<ALN>(g, bi, first, last);
     const bool active = n0 < g.N;
     const Rows qs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 0) : grid_rows(g, pl, q, g.tstride), ds = grid_rows(g, pl, dout, g.C);
     const uint2 *const ex = ext + (int64_t)pl.u * g.N;
-    bf16x8 Kb[2][K / 16], Vb[2][K / 16];
+    bf16x8 Kb[QB][K / 16], Vb[QB][K / 16];
     Mover<LP, W, SRC, SG, true, ALN> mv;
     {
         Held<LP> hk, hv;
@@ -678,20 +733,20 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
         hold<LP, SRC, ALN>(hv, g, bi, pl.win, SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 2) : grid_rows(g, pl, v, g.tstride), n0);
         mv.request(g, bi, pl.win, qs, ds, ex, 0);
         bf16_t *area = S + wave * 64 * (K + 8);
-        operands<K, LP, SRC>(hk, g, area, Kb, FixPair<K>{kOnes});
-        operands<K, LP, SRC>(hv, g, area, Vb, FixPair<K>{kOnes});
+        operands<K, LP, SRC, QB>(hk, g, area, Kb, sel, FixPair<K>{kOnes});
+        operands<K, LP, SRC, QB>(hv, g, area, Vb, sel, FixPair<K>{kOnes});
     }
-    int mylin[2];
+    int mylin[QB];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        const int n = n0 + b * 32 + col;
+    for (int b = 0; b < QB; ++b) {
+        const int n = n0 + (sel + b) * 32 + col;
         mylin[b] = cell_of<ALN>(g, bi, n < g.N ? n : g.N - 1).lin(bi);
     }
     __syncthreads();
     init_cols<K, K>(g, S, false, true, false, NT);
-    f32x16 Ak[2][DB], Av[2][DB];
+    f32x16 Ak[QB][DB], Av[QB][DB];
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < QB; ++b)
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -700,7 +755,7 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
     const int tro = tr_lane_offset<I::XS>(lane), ako = col * I::XS + 8 * hf;
     const float scale = bi.qs;
     const f32x16 z = {0};
-    f32x16 next;            // (ALN) the bias of block (1, the coming one)
+    f32x16 next;            // (CARRY) the bias of block (1, the coming one)
     mv.template commit<K, K, false>(g, bi, S, 0, scale);
     mv.request(g, bi, pl.win, qs, ds, ex, ntiles > 1 ? 1 : 0);
     for (int t0 = 0, t1, end = strip_tiles; t0 < ntiles; t0 = t1) {
@@ -708,7 +763,7 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
         const Chunk ch = chunk_of<ALN>(g, bi, t0, t1, span);
         stage_bias<1>(g, bi, ch, pl.hd, bi.bs, B, NT);
         __syncthreads();
-        if (ALN && t0 * kTile == ch.t0 && active) next = bias_block<ALN>(B + ch.c0 - mylin[1], words_of<ALN>(bi, ch, nullptr, t0, 0, hf));
+        if (CARRY && t0 * kTile == ch.t0 && active) next = bias_block<ALN>(B + ch.c0 - mylin[QB - 1], words_of<ALN>(bi, ch, nullptr, t0, 0, hf));
         for (int tile = t0; tile < t1; ++tile) {
             const bf16_t *cur = S + (tile & 1) * I::STAGE;
             if (tile + 1 < ntiles) {
@@ -717,7 +772,8 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
             }
             if (active) {
 #pragma unroll
-                for (int qb = 0; qb < 2; ++qb) {
+                for (int qx = 0; qx < (SPLIT ? 1 : 2); ++qx) {
+                    const int qb = SPLIT ? half : qx;
                     if (!ALN && tile * kTile + qb * 32 >= g.N) break;
                     const Words16<ALN> wd = words_of<ALN>(bi, ch, (const int *)(cur + I::LT), tile, qb, hf);
                     bf16x8 Aq[K / 16], Ad[K / 16], Tq[DB][2], Td[DB][2];
@@ -731,10 +787,10 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
                             Td[db][i] = read_tr<I::YS>(cur + I::YR + (qb * 32 + 16 * i) * I::YS, tro, 32 * db);
                         }
 #pragma unroll
-                    for (int bx = 0; bx < 2; ++bx) {
-                        const int b = 1 - bx;
-                        f32x16 s = ALN && b == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[b], wd), p = z;
-                        if (ALN && b == 0) next = s;
+                    for (int bx = 0; bx < QB; ++bx) {
+                        const int b = QB - 1 - bx;
+                        f32x16 s = CARRY && b == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[b], wd), p = z;
+                        if (CARRY && b == 0) next = s;
 #pragma unroll
                         for (int i = 0; i < K / 16; ++i) s = mfma(Aq[i], Kb[b][i], s);
 #pragma unroll
@@ -761,9 +817,14 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
         }
         if (t1 == end) end += strip_tiles;
     }
+    if constexpr (SPLIT) {
+        join<DB>(Ak[0], (float *)S, half);
+        join<DB>(Av[0], (float *)S, half);
+        if (half) return;
+    }
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        const int n = n0 + b * 32 + col;
+    for (int b = 0; b < QB; ++b) {
+        const int n = n0 + (sel + b) * 32 + col;
         if (n >= g.N) continue;
         const int64_t at = (pl.img + pixel(pl.win, cell_of<ALN>(g, bi, n))) * g.C + pl.hd * g.d;
 #pragma unroll
@@ -778,31 +839,31 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
 
 constexpr size_t kBiasBytes = 36 * 1024, kHistBytes = 9 * 1024;
 
-template <int KX, int DB, bool SUM, int SRC, bool ALN, int W>
+template <int KX, int DB, bool SUM, int SRC, bool ALN, bool SPLIT, int W>
 hipError_t launch_fwd_one(const Geo &g, const FwdArgs &a)
 {
     Bias bi{a.bias};
     plan_scale(g, &bi);
-    plan_chunks(g, RIB_BF16, &bi, ALN, false, kBiasBytes, 0);
-    const int nblk = (g.N + 64 * W - 1) / (64 * W);
+    plan_chunks(g, RIB_BF16, &bi, ALN, SPLIT ? 64 : 64 * W, false, kBiasBytes, 0);
+    const int nblk = (g.N + (SPLIT ? 64 : 64 * W) - 1) / (SPLIT ? 64 : 64 * W);
     const size_t smem = stage_bytes<KX, 32 * DB, W>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.ws * 4;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
-    auto kern = fwd_kernel<KX, DB, SUM, SRC, ALN, W>;
+    auto kern = fwd_kernel<KX, DB, SUM, SRC, ALN, SPLIT, W>;
     const hipError_t e = prepare_kernel((const void *)kern, nullptr);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * nblk)), dim3(64 * W), smem, a.st, g, bi, nblk, a.force_max, (const bf16_t *)a.q,
                        (const bf16_t *)a.k, (const bf16_t *)a.v, (bf16_t *)a.out, a.lse);
     return hipGetLastError();
 }
-template <int K, int DB, int SRC, int SG, bool ALN, int W, bool HIST>
+template <int K, int DB, int SRC, int SG, bool ALN, bool SPLIT, int W, bool HIST>
 hipError_t launch_dq_one(const Geo &g, const BwdArgs &a, const Ws &ws)
 {
     Bias bi{a.bias};
     plan_scale(g, &bi);
-    plan_chunks(g, RIB_BF16, &bi, ALN, HIST, kBiasBytes, kHistBytes);
+    plan_chunks(g, RIB_BF16, &bi, ALN, SPLIT ? 64 : 64 * W, HIST, kBiasBytes, kHistBytes);
     const size_t smem = stage_bytes<K, K, W>() + 8 * (size_t)g.M + ((size_t)bi.rows * bi.ws + 1) / 2 * 8 + (size_t)W * bi.hrows * bi.ws * 8;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
-    auto kern = dq_kernel<K, DB, SRC, SG, ALN, W, HIST>;
+    auto kern = dq_kernel<K, DB, SRC, SG, ALN, SPLIT, W, HIST>;
     const hipError_t e = prepare_kernel((const void *)kern, nullptr);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * ws.nblk)), dim3(64 * W), smem, a.st, g, bi, ws.nblk, (const bf16_t *)a.q,
@@ -810,18 +871,19 @@ hipError_t launch_dq_one(const Geo &g, const BwdArgs &a, const Ws &ws)
                        (bf16_t *)a.dq, (uint2 *)((char *)a.ws + ws.ext), (float *)((char *)a.ws + ws.part));
     return hipGetLastError();
 }
-template <int K, int DB, int SRC, int SG, bool ALN, int W>
+template <int K, int DB, int SRC, int SG, bool ALN, bool SPLIT, int W>
 hipError_t launch_pair(const Geo &g, const BwdArgs &a, Ws &ws)
 {
     ws.strips = ALN;
-    hipError_t e = a.dbias != nullptr ? launch_dq_one<K, DB, SRC, SG, ALN, W, true>(g, a, ws) : launch_dq_one<K, DB, SRC, SG, ALN, W, false>(g, a, ws);
+    if (ws.group != (SPLIT ? 64 : 64 * W)) return hipErrorInvalidValue;
+    hipError_t e = a.dbias != nullptr ? launch_dq_one<K, DB, SRC, SG, ALN, SPLIT, W, true>(g, a, ws) : launch_dq_one<K, DB, SRC, SG, ALN, SPLIT, W, false>(g, a, ws);
     if (e != hipSuccess) return e;
     Bias bi{a.bias};
     plan_scale(g, &bi);
-    plan_chunks(g, RIB_BF16, &bi, ALN, false, kBiasBytes, 0);
+    plan_chunks(g, RIB_BF16, &bi, ALN, SPLIT ? 64 : 64 * W, false, kBiasBytes, 0);
     const size_t smem = stage_bytes<K, K, W>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.ws * 4;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
-    auto kern = dkv_kernel<K, DB, SRC, SG, ALN, W>;
+    auto kern = dkv_kernel<K, DB, SRC, SG, ALN, SPLIT, W>;
     e = prepare_kernel((const void *)kern, nullptr);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * ws.nblk)), dim3(64 * W), smem, a.st, g, bi, ws.nblk, (const bf16_t *)a.q,

@@ -480,13 +480,17 @@ hipError_t launch_fwd_src(const Geo &g, const FwdArgs &a)
 {
     if (g.N <= 64) return launch_fwd_small<KX, DB, SUM, SRC>(g, a);
     const int waves = group_waves(RIB_BF16, g.N);
+    const bool split = splits(g, RIB_BF16);
     if constexpr (SRC == kFast) {
         if (strip_shift(RIB_BF16, g.M) >= 0)
-            return waves == 3 ? launch_fwd_one<KX, DB, SUM, SRC, true, 3>(g, a) : launch_fwd_one<KX, DB, SUM, SRC, true, 4>(g, a);
+            return split        ? launch_fwd_one<KX, DB, SUM, SRC, true, true, 4>(g, a)
+                   : waves == 3 ? launch_fwd_one<KX, DB, SUM, SRC, true, false, 3>(g, a)
+                                : launch_fwd_one<KX, DB, SUM, SRC, true, false, 4>(g, a);
     }
-    return waves == 2   ? launch_fwd_one<KX, DB, SUM, SRC, false, 2>(g, a)
-           : waves == 3 ? launch_fwd_one<KX, DB, SUM, SRC, false, 3>(g, a)
-                        : launch_fwd_one<KX, DB, SUM, SRC, false, 4>(g, a);
+    return split        ? launch_fwd_one<KX, DB, SUM, SRC, false, true, 4>(g, a)
+           : waves == 2 ? launch_fwd_one<KX, DB, SUM, SRC, false, false, 2>(g, a)
+           : waves == 3 ? launch_fwd_one<KX, DB, SUM, SRC, false, false, 3>(g, a)
+                        : launch_fwd_one<KX, DB, SUM, SRC, false, false, 4>(g, a);
 }
 
 template <int K, int DB, int SRC, int SG>
@@ -494,13 +498,17 @@ hipError_t launch_bwd_src(const Geo &g, const BwdArgs &a, Ws &ws)
 {
     if (g.N <= 64) return launch_bwd_small<K, DB, SRC, SG>(g, a, ws);
     const int waves = group_waves(RIB_BF16, g.N);
+    const bool split = splits(g, RIB_BF16);
     if constexpr (SG == kFast) {
         if (strip_shift(RIB_BF16, g.M) >= 0)
-            return waves == 3 ? launch_pair<K, DB, SRC, SG, true, 3>(g, a, ws) : launch_pair<K, DB, SRC, SG, true, 4>(g, a, ws);
+            return split        ? launch_pair<K, DB, SRC, SG, true, true, 4>(g, a, ws)
+                   : waves == 3 ? launch_pair<K, DB, SRC, SG, true, false, 3>(g, a, ws)
+                                : launch_pair<K, DB, SRC, SG, true, false, 4>(g, a, ws);
     }
-    return waves == 2   ? launch_pair<K, DB, SRC, SG, false, 2>(g, a, ws)
-           : waves == 3 ? launch_pair<K, DB, SRC, SG, false, 3>(g, a, ws)
-                        : launch_pair<K, DB, SRC, SG, false, 4>(g, a, ws);
+    return split        ? launch_pair<K, DB, SRC, SG, false, true, 4>(g, a, ws)
+           : waves == 2 ? launch_pair<K, DB, SRC, SG, false, false, 2>(g, a, ws)
+           : waves == 3 ? launch_pair<K, DB, SRC, SG, false, false, 3>(g, a, ws)
+                        : launch_pair<K, DB, SRC, SG, false, false, 4>(g, a, ws);
 }
 template <int K, int DB, int SG>
 hipError_t launch_bwd(const Geo &g, const BwdArgs &a, Ws &ws)

@@ -34,6 +34,7 @@ struct Bias {
     uint32_t inv_strip, inv_ws;     // n / strip == mulhi(n, inv_strip)
 };
 // Waves a workgroup: 4, or 3 or 2 where that leaves fewer of them idle at a window's end; 1 where one holds the window.
+constexpr int kSplitGroups = 160;
 constexpr int wave_tokens(int dtype) { return dtype == RIB_BF16 ? 64 : 32; }
 constexpr int group_waves(int dtype, int N)
 {
@@ -42,12 +43,22 @@ constexpr int group_waves(int dtype, int N)
     if (dtype != RIB_BF16) return 4;
     return nb == 2 ? 2 : (nb + 2) / 3 * 3 < (nb + 3) / 4 * 4 ? 3 : 4;
 }
-constexpr int group_tokens(int dtype, int N) { return group_waves(dtype, N) * wave_tokens(dtype); }
+// Whether four waves share 64 stationary tokens (bf16): four times as many workgroups, for grids that would leave most of the chip's 256 compute
+// units without one.  By sizes alone (workgroups of 4 x 64 tokens: us of a forward, forward + backward with its bias gradient, unsplit /
+// split): 32 x 32 windows, 4: 23 / 14, 105 / 67; 96: 24 / 20, 110 / 90; 120: 24 / 19, 111 / 91; 240: 26 / 27, 117 / 139; 64 x 64 windows, 32: 75 /
+// 41, 338 / 192; 192: 80 / 71, 360 / 361; one 96 x 96 window of 6 heads, 216: 176 / 214, 773 / 974.
+inline bool splits(const Geo &g, int dtype)
+{
+    const int sb = group_waves(dtype, g.N) * wave_tokens(dtype);
+    return dtype == RIB_BF16 && g.N > 64 && g.units * ((g.N + sb - 1) / sb) <= kSplitGroups;
+}
+// Stationary tokens a workgroup.
+inline int group_tokens(const Geo &g, int dtype) { return splits(g, dtype) ? 64 : group_waves(dtype, g.N) * wave_tokens(dtype); }
 // Whether windows of this side are walked in strips, and of how many columns (a power of two): where workgroups do not cross them.
 inline int strip_shift(int dtype, int M)
 {
     const int sh = M % 32 == 0 ? 5 : M % 16 == 0 ? 4 : M % 8 == 0 ? 3 : -1;
-    return sh >= 0 && (M << sh == M * M || (M << sh) % group_tokens(dtype, M * M) == 0) ? sh : -1;
+    return sh >= 0 && (M << sh == M * M || (M << sh) % (group_waves(dtype, M * M) * wave_tokens(dtype)) == 0) ? sh : -1;
 }
 inline void plan_order(const Geo &g, int dtype, Bias *b, bool strips)
 {
@@ -164,10 +175,10 @@ __device__ __forceinline__ void stage_bias(const Geo &g, const Bias &b, const Ch
     }
 }
 
-// Adds the waves' histograms of a chunk (dS summed by offset, `hsize` values a wave, WT stationary tokens each) in their order, writes
+// Adds the waves' histograms of a chunk (dS summed by offset, `hsize` values a wave, WT stationary tokens each, STEP from one wave's to the next's) in their order, writes
 // them to the workgroup's sums `dst` (of this streamed strip, from the chunk's first row on) and clears them.  `before`: the last row of
 // the strip's chunk before (-1: none); what that one touched is added to.
-template <bool STRIPS, int W, int WT>
+template <bool STRIPS, int W, int STEP, int WT>
 __device__ __forceinline__ void flush(const Geo &g, const Bias &b, const Chunk &ch, double *H, int hsize, int first, int before, float *dst)
 {
     const int old = before < 0 ? 0 : (before - ch.t.y0 + ch.s.y1 - ch.s.y0 + 1) * b.ws;
@@ -175,7 +186,7 @@ __device__ __forceinline__ void flush(const Geo &g, const Bias &b, const Chunk &
         double sum = 0.;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            const int f = first + w * WT;
+            const int f = first + w * STEP;
             if (f >= g.N) break;
             const Span v = span_of<STRIPS>(g, b, f, f + WT < g.N ? f + WT - 1 : g.N - 1);
             const int at = e - (ch.s.y1 - v.y1) * b.ws;
@@ -238,7 +249,7 @@ hipError_t launch_unpack(const Geo &g, int dtype, const uint8_t *ckpt, void *q, 
 // the first kernel, sums of dS by offset.
 struct Ws {
     size_t ext, part, total;
-    int nblk;                           // workgroups a unit
+    int group, nblk;                    // stationary tokens a workgroup, workgroups a unit
     int words;                          // of a workgroup's sums at most
     bool strips;                        // how the first kernel walked the windows
     int shares;                         // sums a head: of windows, or of the runs of windows a wave takes
@@ -246,7 +257,8 @@ struct Ws {
 inline Ws ws_layout(const Geo &g, int dtype)
 {
     Ws w;
-    const int sb = group_tokens(dtype, g.N);
+    const int sb = group_tokens(g, dtype);
+    w.group = sb;
     w.nblk = (g.N + sb - 1) / sb;
     w.words = 0;
     for (int strips = 0; strips < 2; ++strips) {        // (which way depends on the tensors' alignment too)
@@ -267,10 +279,10 @@ inline Ws ws_layout(const Geo &g, int dtype)
 hipError_t launch_reduce(const Geo &g, int dtype, const Ws &w, const float *part, float *dbias, hipStream_t st);
 
 // Tiles a chunk and the rows that go with it: as many tiles as fit `bias_bytes` of bias and (hist) `hist_bytes` a wave, of one strip.
-inline void plan_chunks(const Geo &g, int dtype, Bias *b, bool strips, bool hist, size_t bias_bytes, size_t hist_bytes)
+inline void plan_chunks(const Geo &g, int dtype, Bias *b, bool strips, int sb, bool hist, size_t bias_bytes, size_t hist_bytes)
 {
     plan_order(g, dtype, b, strips);
-    const int sb = group_tokens(dtype, g.N), ntiles = (b->strip + kTile - 1) / kTile;
+    const int ntiles = (b->strip + kTile - 1) / kTile;
     const int srows = most_rows(sb, g, *b), wrows = most_rows(wave_tokens(dtype), g, *b);
     b->prows = g.M - 1 + srows;
     for (int tiles = ntiles;; tiles = tiles > 8 ? tiles - tiles / 8 : tiles - 1) {

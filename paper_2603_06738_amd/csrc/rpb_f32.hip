@@ -361,7 +361,7 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
             __syncthreads();
         }
         if (HIST) {
-            flush<ALN, W, 32>(g, bi, ch, H, hsize, first, before,
+            flush<ALN, W, 32, 32>(g, bi, ch, H, hsize, first, before,
                               part + sums_at(g, bi, pl.u, nblk, pl.blk, bi.prows, ch.t.x0) + ch.t.y0 * bi.ws);
             before = t1 == end ? -1 : ch.t.y1;
         }
@@ -458,7 +458,7 @@ template <int DB, bool ALN, int W>
 hipError_t launch_fwd_one(const Geo &g, const FwdArgs &a)
 {
     Bias bi{a.bias};
-    plan_chunks(g, RIB_F32, &bi, ALN, false, kBiasBytes, 0);
+    plan_chunks(g, RIB_F32, &bi, ALN, 32 * W, false, kBiasBytes, 0);
     const int nblk = (g.N + 32 * W - 1) / (32 * W);
     const size_t smem = stage_bytes<DB>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.ws * 4;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
@@ -480,7 +480,7 @@ template <int DB, bool CKPT, bool ALN, int W, bool HIST>
 hipError_t launch_dq_one(const Geo &g, const BwdArgs &a, const Ws &ws)
 {
     Bias bi{a.bias};
-    plan_chunks(g, RIB_F32, &bi, ALN, HIST, kBiasBytes, kHistBytes);
+    plan_chunks(g, RIB_F32, &bi, ALN, 32 * W, HIST, kBiasBytes, kHistBytes);
     const size_t smem = stage_bytes<DB>() + 8 * (size_t)g.M + ((size_t)bi.rows * bi.ws + 1) / 2 * 8 + (size_t)W * bi.hrows * bi.ws * 8;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
     auto kern = dq_kernel<DB, CKPT, ALN, W, HIST>;
@@ -498,7 +498,7 @@ hipError_t launch_pair(const Geo &g, const BwdArgs &a, Ws &ws)
     hipError_t e = a.dbias != nullptr ? launch_dq_one<DB, CKPT, ALN, W, true>(g, a, ws) : launch_dq_one<DB, CKPT, ALN, W, false>(g, a, ws);
     if (e != hipSuccess) return e;
     Bias bi{a.bias};
-    plan_chunks(g, RIB_F32, &bi, ALN, false, kBiasBytes, 0);
+    plan_chunks(g, RIB_F32, &bi, ALN, 32 * W, false, kBiasBytes, 0);
     const size_t smem = stage_bytes<DB>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.ws * 4;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
     auto kern = dkv_kernel<DB, CKPT, ALN, W>;

@@ -120,12 +120,12 @@ hipError_t launch_reduce(const Geo &g, int dtype, const Ws &w, const float *part
     const int L = (2 * g.M - 1) * (2 * g.M - 1);
     Bias bi{};
     plan_order(g, dtype, &bi, w.strips);
-    bi.prows = g.M - 1 + most_rows(group_tokens(dtype, g.N), g, bi);
+    bi.prows = g.M - 1 + most_rows(w.group, g, bi);
     const int windows = w.shares;
     int runs = 16;
     while (runs > 1 && (runs > windows || (runs / 2 >= windows && w.nblk > 1))) runs /= 2;
     hipLaunchKernelGGL(reduce_kernel, dim3((L + 63) / 64, g.heads), dim3(1024), 0, st, g, bi, windows, runs, w.nblk,
-                       group_tokens(dtype, g.N), part, dbias);
+                       w.group, part, dbias);
     return hipGetLastError();
 }
 hipError_t launch_table_fwd(int M, int heads, int buckets, int dtype, const void *table, const int32_t *index, float *bias, hipStream_t st)

@@ -6,7 +6,8 @@ Bounds are per element: every input of a sum moves by its own relative error, so
 |term| times that error.  u is half a step of the operands' type: bf16 2^-8, fp32 2^-24.
 
     Q times scale is rounded once           a logit moves by at most eps_ij = u * scale * sum_c |q_ic k_jc|
-    P = exp(S - LSE), LSE of those logits   a probability by at most 2 max_j eps_ij (S by one, LSE by one), relative
+    P = exp(S - LSE), LSE of those logits   a probability by at most 2 max_j eps_ij (S by one, LSE by one), relative, and by u: LSE's
+                                            denominator adds up probabilities as rounded, log sum p (1 + t) with |t| <= u
     P and dS are rounded for the products   u more; Q's own rounding enters dK once more; outputs are rounded: u
     bf16 keeps -LSE and -delta as two parts 2^-16 of each
     fp32 sums of n terms                    n 2^-24
@@ -129,7 +130,7 @@ def attention(q, k, v, bias, heads, M, s, scale, u, out=None, dout=None, bwd_qkv
                     dP = do @ vv.T
                     dS = P * (dP - delta)
                     # P's relative error, and what dP - delta is off by
-                    t = 1.1 * (2 * eps + split * (1 + np.abs(np.where(full, lse, 0.0))) + add)
+                    t = 1.1 * (2 * eps + u + split * (1 + np.abs(np.where(full, lse, 0.0))) + add)
                     off = (split * np.abs(delta) + 2.0 ** -24 * (d + 4) * (np.abs(do) @ np.abs(vv).T + np.abs(do * o).sum(1, keepdims=True)))
                     eS = t * np.abs(dS) + 1.1 * P * off
                     r = u + add
