@@ -262,20 +262,20 @@ rib_status rib_features_bwd(const rib_gen_params *p, const float *W_h, const flo
  *
  * EXCLUDED PAIRS.  A bias of minus infinity, or any at or below -1e30 (so also the lowest value of a type), excludes the pairs of its
  * offset: their probability and their gradients are exactly zero.  A row whose pairs are all excluded gives O = 0,
- * LSE = minus infinity and adds nothing to any gradient.  (An infinity or NaN in q, k, v or d_out spreads over its own
- * (window, head), excluded pairs too, and through the sum over windows into dbias.)
+ * LSE = minus infinity and adds nothing to any gradient.  (An infinity or NaN in q, k, v or d_out may spread over its
+ * own (window, head), excluded pairs too, and through the sum over windows into dbias.)
  *
- * rib_params: r must be 0 and flags 0 or RIB_FLAG_FORCE_ROW_MAX (else RIB_ERR_UNSUPPORTED); scale_p is not used.  bf16 tensors
- * may lie on 2-byte boundaries and have any d of 1..64 and any token_stride; even d >= 8, even strides and 4-byte boundaries are
- * the fast case.  Everything runs on the matrix cores: bf16 storage with bf16 operands (Q times scale_c and P and dS rounded to
- * nearest) and fp32 sums, fp32 storage in fp32. */
+ * rib_params: r must be 0, flags 0 or RIB_FLAG_FORCE_ROW_MAX, heads at most 65535 (else RIB_ERR_UNSUPPORTED); scale_p is not used.
+ * Tensors may lie on boundaries of their own type (bf16: 2 bytes) and have any d of 1..64 and any token_stride; even d >= 8, even
+ * strides and 4-byte boundaries are the fast case in bf16.  Everything runs on the matrix cores: bf16 storage with bf16 operands, of which P
+ * and dS are rounded to nearest (logits are not: they are sums of exact products, scaled in fp32), and fp32 sums; fp32 storage in fp32. */
 
 /* Forward.  bias [heads][(2M-1)^2] fp32 (from rib_rpb_table_fwd, or the caller's own); everything else as rib_window_attn_fwd. */
 rib_status rib_rpb_attn_fwd(const rib_params *p, const void *q, const void *k, const void *v, const float *bias,
                             void *out, float *lse, void *stream);
 
-/* Bytes of device scratch the backward needs (0 if the parameters are invalid): 8 a (token, head), and the
- * partial sums of dbias of every 256 (bf16) or 128 (fp32) tokens of a window and head. */
+/* Bytes of device scratch the backward needs (0 if the parameters are invalid): 8 a (token, head), and
+ * partial sums of dbias of every 64 to 256 tokens of a window and head. */
 size_t rib_rpb_attn_bwd_workspace_bytes(const rib_params *p);
 
 /* Backward: the probabilities are made again from q, k, bias and lse,
@@ -285,7 +285,7 @@ size_t rib_rpb_attn_bwd_workspace_bytes(const rib_params *p);
  *     dbias[head][o] = sum over images, windows and the pairs of offset o of dS
  * dq, dk, dv [B][H][W][C] (dense, dtype of q) and dbias [heads][(2M-1)^2] fp32 are OVERWRITTEN; dbias may be NULL (a bias that is not
  * trained), which saves its sums.  No result depends on the order in which workgroups run: results are run-to-run
- * identical.  `workspace`: as for rib_window_attn_bwd, of rib_rpb_attn_bwd_workspace_bytes(p) bytes. */
+ * identical (on one kind of GPU: windows of up to 64 tokens are shared out by its number of compute units).  `workspace`: as for rib_window_attn_bwd, of rib_rpb_attn_bwd_workspace_bytes(p) bytes. */
 rib_status rib_rpb_attn_bwd(const rib_params *p, const void *q, const void *k, const void *v, const float *bias,
                             const void *out, const void *d_out, const float *lse, void *dq, void *dk, void *dv, float *dbias,
                             void *workspace, size_t workspace_bytes, void *stream);

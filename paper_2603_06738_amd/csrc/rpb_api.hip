@@ -22,7 +22,7 @@ rib_status attn_geo(const rib_params *p, Geo *g)
 {
     const rib_status st = make_geo(p, g);
     if (st != RIB_OK) return st;
-    if (p->r != 0 || (p->flags & ~RIB_FLAG_FORCE_ROW_MAX) != 0) return RIB_ERR_UNSUPPORTED;
+    if (p->r != 0 || (p->flags & ~RIB_FLAG_FORCE_ROW_MAX) != 0 || p->heads > 65535) return RIB_ERR_UNSUPPORTED;
     return RIB_OK;
 }
 rib_status check_table(const rib_rpb_params *p)

@@ -3,14 +3,23 @@
 //
 // A wave owns 64 stationary tokens as MFMA B operands, a workgroup W waves; the other side of the unit streams through LDS in
 // tiles of 64 token rows, two stages in turn.  (SPLIT, for grids that would leave most of the chip idle: four waves share 64 stationary
-// tokens, two blocks of them by two of every tile's; the sums of a block's two waves are added through LDS at the end.)  Scores are 32x32 blocks with the streamed tokens as rows, so a lane owns one
-// stationary token and 16 streamed ones; their bias is the C operand of the score product.  What is packed to bf16 there
+// tokens, two blocks of them by two of every tile's; the sums of a block's two waves are added through LDS at the end.)  Scores are
+// 32x32 blocks with the streamed tokens as rows, so a lane owns one stationary token and 16 streamed ones; their bias is the C operand
+// of the score product.  What is packed to bf16 there
 // (P, dS) is the B operand of the product that contracts over the streamed tokens, whose A operand is read transposed from
 // the same rows.  Products of q and k are exact in fp32 and scaled there: rounding a scaled q to bf16 would save 16 of some 100 vector
-// instructions a block, and cost as much accuracy as the rounding of P.
+// instructions a block, and cost as much accuracy as the rounding of P (2-norm errors of a training step 2.5e-3 so, 3.4e-3 with it; forward 8 %,
+// whole step 5 % slower).
 //
 // The backward's -delta rides in two more columns of dO's rows, as a bf16 pair (high and low part, 2^-16 of it is lost), against
-// ones in V's: the product is then dP - delta.  Where the query is streamed (dkv), -LSE does the same beside q and k.
+// ones in V's: the product is then dP - delta.  Where the query is streamed (dkv), -LSE does the same beside q and k.  LSE's denominator is
+// the sum of P as rounded (a column of ones in V), which O wants, and which moves LSE by 2^-8 at most, in a row of few keys.
+//
+// What bounds it, by counters (16 images of 96 x 96, 32 x 32 windows, 6 heads of 30; forward / dq / dkv 194 / 394 / 315 us): the vector issue is
+// busy 60 % of the time and the matrix pipe 29 / 20 / 35 %, and the two hardly overlap.  A block of the forward has 60 vector instructions,
+// 40 of them exp2, scale and pack.  Parts taken out, us: staging -20 / -32 / -39, the barriers too -22 / -43 / -46, the bias -18 / -17 / -14.  Three
+// waves a SIMD (168 registers) in the forward up to 32 channels, two elsewhere.  Tiles of 128 tokens (half the barriers): forward the same, dq 5 %
+// slower.
 #pragma once
 
 #include "rpb_common.h"

@@ -6,7 +6,7 @@
 // and dv, whose other sides wait in registers; scores and exponentials are made in both layouts, which is cheaper than turning them in LDS.  Nothing
 // is shared between waves, so nothing waits for another; bias and histogram stay in LDS over the wave's windows.
 // Forward + backward of 32 images of 56 x 56, 7 x 7 windows, 3 heads of 32, us, as two tiled kernels and a forward in single-wave
-// workgroups / here: kernels 180 / SMALLUS.
+// workgroups / here: kernels 180 / 108.
 #pragma once
 
 #include "rpb_bf16.h"

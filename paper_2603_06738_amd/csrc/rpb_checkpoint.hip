@@ -3,7 +3,8 @@
 // A (tensor, unit, token) row of d values becomes dp = 16 ceil(d / 16) codes and an exponent byte e: value = (code - 128) 2^(e - 127), e
 // the smallest for which the row's largest fits 127 steps.  Codes lie in the units' own token order, so what the backward
 // reads of a unit is contiguous.  Codes under a power of two are exact in either storage type.
-// Bound by memory: q, k, v read once and a little over half of that (bf16; a quarter, fp32) written.
+// Bound by memory: q, k, v read once and a little over half of that (bf16; a quarter, fp32) written.  16 images of 96 x 96, 6 heads of 30, bf16:
+// 76 us, 247 MB, 3.2 TB/s of the 5.1 a copy reaches (a head at a time, rows in 16 lanes 256 us, in 4 lanes 90).
 #include "rpb_common.h"
 
 namespace rib {

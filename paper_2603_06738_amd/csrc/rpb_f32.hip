@@ -5,7 +5,8 @@
 // stages in turn.  Scores have the streamed tokens as rows: a lane owns one stationary token and 16 streamed ones, and its
 // P and dS are, register by register, the B operands of the product that contracts over the streamed tokens (k = 0 and 1 of
 // an instruction are the two lane halves).  What bounds it is that instruction: a 32x32 block at 32 channels is 16 of them
-// a product (64 clk each), the exponentials beside it a tenth.
+// a product (64 clk each), the exponentials beside it a tenth.  By counters (4 images of 96 x 96, 32 x 32 windows, 6 heads of 30; forward / dq / dkv
+// 318 / 504 / 515 us) it is busy 65 / 59 / 76 % of the time; the rest is starts, ends and barriers.
 #include "rpb_bf16.h"
 
 namespace rib {

@@ -29,7 +29,7 @@ __global__ __launch_bounds__(256) void table_fwd_kernel(int L, int buckets, cons
 // bucket whose gradient is 2^-21 of the largest still has 24 bits.  Values that are not finite are noted by kind beside the sums.
 constexpr int kBuckets = 2048;          // buckets a workgroup at most
 // Every workgroup of a head reads all offsets and adds those of its `chunk` buckets: the conversions, not the reads, are what costs
-// (36481 offsets in 625 buckets, us: 36 in one workgroup a head, TABLEUS in 16).
+// (36481 offsets in 625 buckets, us: 36 in one workgroup a head, 15 in 16).
 template <class T>
 __global__ __launch_bounds__(1024) void table_bwd_kernel(int L, int buckets, int chunk, int bits, const float *__restrict__ dbias,
                                                          const int32_t *__restrict__ index, T *__restrict__ dtable)

@@ -56,7 +56,7 @@ def test_bad_types_and_what_is_not_built():
     for call in (fwd, bwd, bwd_ckpt):
         assert call(good(dtype=7)) == 3
         assert call(None) == 1
-        for kw in (dict(d=65), dict(r=2), dict(flags=rb.RIB_FLAG_VECTOR_ONLY), dict(flags=rb.RIB_FLAG_WIDE), dict(H=257, W=257, window=257)):
+        for kw in (dict(d=65), dict(r=2), dict(flags=rb.RIB_FLAG_VECTOR_ONLY), dict(flags=rb.RIB_FLAG_WIDE), dict(H=257, W=257, window=257), dict(heads=65536, d=1)):
             assert call(good(**kw)) == 4, kw
     assert fwd(good(flags=64)) == 2
     assert rb.rib_rpb_attn_bwd_workspace_bytes(good(r=2)) == 0
