@@ -137,7 +137,9 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
         lay<LP, SRC, KY, false>(hv, g, Y, 1.f);
         if (w + 1 < sh.w1) request(w + 1);
         f32x16 O[2][DB];
-        float sum[2] = {0.f, 0.f}, top[2] = {0.f, 0.f};
+        // `sum`: of P as rounded where V has a column of ones, which O wants; `exact`: of P before it is rounded, which LSE wants (with few keys
+        // the other would move it by up to 2^-8)
+        float sum[2] = {0.f, 0.f}, top[2] = {0.f, 0.f}, exact[2] = {0.f, 0.f};
         // all keys of a block of queries at once: scores first, so that their maximum is at hand where it is wanted
         auto walk = [&](bool max) {
 #pragma unroll
@@ -167,7 +169,7 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
                     m = fmaxf(m, __shfl_xor(m, 32));
                     top[qb] = m == -INFINITY ? 0.f : m;         // (a row without a key: any finite stabiliser does)
                 }
-                sum[qb] = 0.f;
+                exact[qb] = 0.f;
 #pragma unroll
                 for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -180,20 +182,19 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
                     for (int i = 0; i < 16; ++i) s[kb][i] = __builtin_amdgcn_exp2f(s[kb][i] - top[qb]);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) P[i] = pack_bf16(s[kb][2 * i], s[kb][2 * i + 1]);
-                    if (SUM) {
-                        float a = 0.f, b = 0.f;
+                    float a = 0.f, b = 0.f;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) a += s[kb][2 * i], b += s[kb][2 * i + 1];
-                        sum[qb] += a + b;
-                    }
+                    for (int i = 0; i < 8; ++i) a += s[kb][2 * i], b += s[kb][2 * i + 1];
+                    exact[qb] += a + b;
 #pragma unroll
                     for (int db = 0; db < DB; ++db) {
                         O[qb][db] = mfma(read_tr<I::YS>(Y + kb * 32 * I::YS, tro, 32 * db), as_bf16x8(P[0], P[1], P[2], P[3]), O[qb][db]);
                         O[qb][db] = mfma(read_tr<I::YS>(Y + (kb * 32 + 16) * I::YS, tro, 32 * db), as_bf16x8(P[4], P[5], P[6], P[7]), O[qb][db]);
                     }
                 }
-                const float mine = SUM ? sum[qb] : O[qb][DB - 1][15], other = __shfl_xor(mine, 32);
-                sum[qb] = SUM ? mine + other : hf ? mine : other;
+                exact[qb] += __shfl_xor(exact[qb], 32);
+                const float mine = O[qb][DB - 1][15], other = __shfl_xor(mine, 32);
+                sum[qb] = SUM ? exact[qb] : hf ? mine : other;
             }
         };
         bool bad = force_max != 0;
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
             if (n >= g.N) continue;
             const float inv = sum[qb] == 0.f ? 0.f : 1.f / sum[qb];
             if (lse != nullptr && hf == 0)
-                lse[((int64_t)w * g.heads + sh.hd) * g.N + n] = sum[qb] == 0.f ? -INFINITY : (top[qb] + __builtin_amdgcn_logf(sum[qb])) * kLn2;
+                lse[((int64_t)w * g.heads + sh.hd) * g.N + n] = sum[qb] == 0.f ? -INFINITY : (top[qb] + __builtin_amdgcn_logf(exact[qb])) * kLn2;
             bf16_t *row = out + (s.img + s.pixel(g, n)) * g.C + sh.hd * g.d;
 #pragma unroll
             for (int db = 0; db < DB; ++db) store_row<SRC>(row, O[qb][db], db, g.d, hf, inv);
