@@ -137,7 +137,7 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
         lay<LP, SRC, KY, false>(hv, g, Y, 1.f);
         if (w + 1 < sh.w1) request(w + 1);
         f32x16 O[2][DB];
-        // `sum`: of P as rounded where V has a column of ones, which O wants; `exact`: of P before it is rounded, which LSE wants (with few keys
+        // `sum`: of P as rounded, which O wants (a column of ones in V has it, where there is one); `exact`: of P before it is rounded, which LSE wants (with few keys
         // the other would move it by up to 2^-8)
         float sum[2] = {0.f, 0.f}, top[2] = {0.f, 0.f}, exact[2] = {0.f, 0.f};
         // all keys of a block of queries at once: scores first, so that their maximum is at hand where it is wanted
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
                     m = fmaxf(m, __shfl_xor(m, 32));
                     top[qb] = m == -INFINITY ? 0.f : m;         // (a row without a key: any finite stabiliser does)
                 }
-                exact[qb] = 0.f;
+                exact[qb] = sum[qb] = 0.f;
 #pragma unroll
                 for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -186,6 +186,12 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
 #pragma unroll
                     for (int i = 0; i < 8; ++i) a += s[kb][2 * i], b += s[kb][2 * i + 1];
                     exact[qb] += a + b;
+                    if (SUM) {
+                        float r = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) r += lo_bf16(P[i]) + hi_bf16(P[i]);
+                        sum[qb] += r;
+                    }
 #pragma unroll
                     for (int db = 0; db < DB; ++db) {
                         O[qb][db] = mfma(read_tr<I::YS>(Y + kb * 32 * I::YS, tro, 32 * db), as_bf16x8(P[0], P[1], P[2], P[3]), O[qb][db]);
@@ -193,8 +199,8 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
                     }
                 }
                 exact[qb] += __shfl_xor(exact[qb], 32);
-                const float mine = O[qb][DB - 1][15], other = __shfl_xor(mine, 32);
-                sum[qb] = SUM ? exact[qb] : hf ? mine : other;
+                const float mine = SUM ? sum[qb] : O[qb][DB - 1][15], other = __shfl_xor(mine, 32);
+                sum[qb] = SUM ? mine + other : hf ? mine : other;
             }
         };
         bool bad = force_max != 0;
