@@ -316,7 +316,8 @@ rib_status rib_rpb_table_bwd(const rib_rpb_params *p, const float *dbias, const 
  * Every row of d values (a token's q, k or v of one head) is kept as codes c of 0..255 under one exponent byte e; they stand for
  *     x = (c - 128) * 2^(e - 127)
  * with the smallest e >= 1 for which the row's largest magnitude is at most 127 * 2^(e - 127), values rounded to the nearest code (ties
- * to even).  A row of zeros has e = 0; a row that holds an infinity or NaN has e = 255 and stands for NaN.  What a checkpoint stands
+ * to even).  e is 248 at most: values above 127 * 2^121 become that, up to a step lower (the next step's codes would stand for numbers
+ * that neither type holds).  A row of zeros has e = 0; a row that holds an infinity or NaN has e = 255 and stands for NaN.  What a checkpoint stands
  * for is exact in bf16 and in fp32, so that packing it again changes nothing.
  * The buffer (device memory, 16-byte aligned): for q, k, v in turn codes [B*nW*heads][N][16 * ceil(d / 16)] (the columns past d stand for
  * zero), units numbered as lse's; then for q, k, v exponent bytes [B*nW*heads][N].

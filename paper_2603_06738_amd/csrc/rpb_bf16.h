@@ -89,12 +89,12 @@ template <int SRC>
 __device__ __forceinline__ Raw widen_piece(const Raw &r)
 {
     if constexpr (SRC != kCkpt) return r;
-    const float s = __uint_as_float(r.w[2] << 23), z = -128.f * s;
+    const float s = code_step(r.w[2]);
     Raw o;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t w = r.w[i >> 1] >> (16 * (i & 1));
-        o.w[i] = trunc_pack(fmaf((float)(w & 255u), s, z), fmaf((float)((w >> 8) & 255u), s, z));
+        o.w[i] = trunc_pack(code_value(w & 255u, s), code_value((w >> 8) & 255u, s));
     }
     return o;
 }

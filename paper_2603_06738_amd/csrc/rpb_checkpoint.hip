@@ -1,7 +1,7 @@
 // 8-bit checkpoints of q, k and v: packed for the backward, and unpacked.  Format: include/rib_attn.h.
 //
 // A (tensor, unit, token) row of d values becomes dp = 16 ceil(d / 16) codes and an exponent byte e: value = (code - 128) 2^(e - 127), e
-// the smallest for which the row's largest fits 127 steps.  Codes lie in the units' own token order, so what the backward
+// the smallest for which the row's largest fits 127 steps (248 at most: above 127 * 2^121 codes stay at 127).  Codes lie in the units' own token order, so what the backward
 // reads of a unit is contiguous.  Codes under a power of two are exact in either storage type.
 // Bound by memory: q, k, v read once and a little over half of that (bf16; a quarter, fp32) written.  16 images of 96 x 96, 6 heads of 30, bf16:
 // 76 us, 247 MB, 3.2 TB/s of the 5.1 a copy reaches (a head at a time, rows in 16 lanes 256 us, in 4 lanes 90).
@@ -98,12 +98,12 @@ __global__ __launch_bounds__(256) void pack_kernel(Geo g, const T *__restrict__ 
         if (big >= 0x7f800000u) e = 255;                        // not finite: the row stands for NaN
         else if (big != 0u) {
             e = (int)(big >> 23) - 6 + ((big & 0x7fffffu) > 0x7e0000u ? 1 : 0);
-            if (e < 1) e = 1;
+            e = e < 1 ? 1 : e > 248 ? 248 : e;                  // (64 steps of 2^122 would be beyond either type)
         }
         const float per = e == 0 || e == 255 ? 0.f : __uint_as_float((uint32_t)(254 - e) << 23);
         uint32_t codes[2] = {0u, 0u};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) codes[i >> 2] |= (uint32_t)((e == 255 ? 0 : (int)rintf(x[i] * per)) + 128) << (8 * (i & 3));
+        for (int i = 0; i < 8; ++i) codes[i >> 2] |= (uint32_t)((e == 255 ? 0 : (int)fminf(fmaxf(rintf(x[i] * per), -127.f), 127.f)) + 128) << (8 * (i & 3));
         if (s.n < 0) continue;
         const int64_t to = s.row + which * rows;
         if (s.c < dp) *(uint2 *)(ckpt + to * dp + s.c) = uint2{codes[0], codes[1]};
@@ -122,12 +122,12 @@ __global__ __launch_bounds__(256) void unpack_kernel(Geo g, const uint8_t *__res
         const Slot s = slot_of<LP>(g, corner, slot);
         if (s.n < 0 || s.c >= g.d) continue;
         const int64_t from = s.row + which * rows;
-        const float sc = __uint_as_float((uint32_t)(ckpt + 3 * rows * dp)[from] << 23), z = -128.f * sc;
+        const float sc = code_step((ckpt + 3 * rows * dp)[from]);
         const uint2 codes = *(const uint2 *)(ckpt + from * dp + s.c);
         T *p = dst + s.at + s.c;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (s.c + i < g.d) store_as(p + i, fmaf((float)(((i < 4 ? codes.x : codes.y) >> (8 * (i & 3))) & 255u), sc, z));
+            if (s.c + i < g.d) store_as(p + i, code_value(((i < 4 ? codes.x : codes.y) >> (8 * (i & 3))) & 255u, sc));
     }
 }
 

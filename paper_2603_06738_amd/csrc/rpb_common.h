@@ -214,6 +214,9 @@ enum Source { kFast = 0, kAny = 1, kCkpt = 2 };
 // Checkpoint (include/rib_attn.h): for q, k and v in turn [units][N][dp] codes; then for each [units][N] exponent bytes.
 __host__ __device__ inline int ckpt_row(int d) { return (d + 15) & ~15; }
 __host__ __device__ inline int64_t ckpt_rows(const Geo &g) { return g.units * g.N; }
+// The step of exponent byte `e`, and what code `c` stands for under it.  (Exact: 128 is taken off first, since 128 steps may pass the largest number.)
+__device__ __forceinline__ float code_step(uint32_t e) { return __uint_as_float(e << 23); }
+__device__ __forceinline__ float code_value(uint32_t c, float step) { return ((float)c - 128.f) * step; }
 
 // Launchers.
 struct FwdArgs {

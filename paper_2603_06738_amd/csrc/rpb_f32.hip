@@ -49,9 +49,8 @@ __device__ __forceinline__ Raw get4(const Rows &s, uint32_t t, int n, int c, int
     if constexpr (CKPT) {
         const int dp = ckpt_row(d);
         const uint32_t w = c < dp ? *(const uint32_t *)(s.base + (int64_t)n * s.stride + c) : 0x80808080u;
-        const float sc = __uint_as_float((uint32_t)s.exps[n] << 23), z = -128.f * sc;
-        return Raw{fmaf((float)(w & 255u), sc, z), fmaf((float)((w >> 8) & 255u), sc, z), fmaf((float)((w >> 16) & 255u), sc, z),
-                   fmaf((float)(w >> 24), sc, z)};
+        const float sc = code_step(s.exps[n]);
+        return Raw{code_value(w & 255u, sc), code_value((w >> 8) & 255u, sc), code_value((w >> 16) & 255u, sc), code_value(w >> 24, sc)};
     } else {
         const float *p = (const float *)(s.base + (int64_t)t * s.stride) + c;
         if (c + 4 <= d) {
