@@ -11,8 +11,9 @@
 // instructions a block, and cost as much accuracy as the rounding of P (2-norm errors of a training step 2.5e-3 so, 3.4e-3 with it; forward 8 %,
 // whole step 5 % slower).
 //
-// The backward's -delta rides in two more columns of dO's rows, as a bf16 pair (high and low part, 2^-16 of it is lost), against
-// ones in V's: the product is then dP - delta.  Where the query is streamed (dkv), -LSE does the same beside q and k.  LSE's denominator is
+// The backward's -delta rides in two more columns of dO's rows, as a bf16 pair (high and low part, 2^-17 of it is lost), against
+// ones in V's: the product is then dP - delta.  LSE is an exponent, where such a loss would grow with it: it stays in fp32, and lies beside the
+// rows in LDS where the query is streamed (dkv).  LSE's denominator is
 // the sum of P as rounded (a column of ones in V), which O wants, and which moves LSE by 2^-8 at most, in a row of few keys.
 //
 // What bounds it, by counters (16 images of 96 x 96, 32 x 32 windows, 6 heads of 30; forward / dq / dkv 194 / 394 / 315 us): the vector issue is
@@ -33,12 +34,12 @@ using namespace rows;
 constexpr uint32_t kOnes = 0x3f803f80u;
 constexpr float kNoRow = 1e30f;         // in place of LSE where a row has no key: every probability is zero
 
-// LDS image of a tile: X and Y rows, a streamed token's lin().  K: columns of the contracted width.
-template <int KX, int KY>
+// LDS image of a tile: X and Y rows, a streamed token's lin() and (EXT) -LSE in base 2.  K: columns of the contracted width.
+template <int KX, int KY, bool EXT = false>
 struct Img {
     static constexpr int XS = KX + 8, YS = KY + 8;
-    static constexpr int YR = kTile * XS, LT = YR + kTile * YS;
-    static constexpr int STAGE = LT + 2 * kTile;                // bf16 elements
+    static constexpr int YR = kTile * XS, LT = YR + kTile * YS, EX = LT + 2 * kTile;
+    static constexpr int STAGE = EX + (EXT ? 2 * kTile : 0);    // bf16 elements
     static constexpr int TOTAL = 2 * STAGE + 32;                // (transposed reads of the last row may run over its end)
 };
 
@@ -136,11 +137,11 @@ struct Mover {
             if (EXT) e[p] = ext[n];
         }
     }
-    // KX, KY: the images' widths.  ONES: ones in the two last columns of both (dq); EXT: -LSE and -delta there (dkv).
+    // KX, KY: the images' widths.  ONES: ones in the two last columns of both (dq); EXT: -delta in Y's (dkv).
     template <int KX, int KY, bool ONES>
     __device__ __forceinline__ void commit(const Geo &g, const Bias &bi, bf16_t *S, int tile, float scale)
     {
-        using I = Img<KX, KY>;
+        using I = Img<KX, KY, EXT>;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const int slot = p * NT + threadIdx.x, row = slot / LP, j = slot % LP;
@@ -156,7 +157,7 @@ struct Mover {
             put_piece<SX>(xr, a, j, g.d);
             put_piece<SY>(yr, b, j, g.d);
             if (EXT && j == 0) {
-                *(uint32_t *)(xr + KX - 2) = in ? e[p].x : pack_bf16(-kNoRow, 0.f);
+                ((float *)(S + I::EX))[row] = in ? __uint_as_float(e[p].x) : -kNoRow;
                 *(uint32_t *)(yr + KY - 2) = in ? e[p].y : 0u;
             }
             if (!ALN && j == 0) ((int *)(S + I::LT))[row] = cell_of<false>(g, bi, in ? n : g.N - 1).lin(bi);
@@ -164,15 +165,15 @@ struct Mover {
     }
 };
 // Columns that no commit writes, once for both stages (beside the first commit: what both write is the same).  `ones`: in the last two
-// columns of X and Y; `ext`: not those columns; `one`: in Y's last column.
-template <int KX, int KY>
-__device__ __forceinline__ void init_cols(const Geo &g, bf16_t *S, bool ones, bool ext, bool one, int nt)
+// columns of X and Y; EXT: not those of Y; `one`: in Y's last column.
+template <int KX, int KY, bool EXT = false>
+__device__ __forceinline__ void init_cols(const Geo &g, bf16_t *S, bool ones, bool one, int nt)
 {
-    using I = Img<KX, KY>;
+    using I = Img<KX, KY, EXT>;
     for (int e = threadIdx.x; e < 2 * kTile; e += nt) {
         bf16_t *xr = S + (e / kTile) * I::STAGE + (e % kTile) * I::XS, *yr = S + (e / kTile) * I::STAGE + I::YR + (e % kTile) * I::YS;
-        for (int c = g.d; c < (ext ? KX - 2 : KX); ++c) xr[c] = ones && c >= KX - 2 ? 0x3f80 : 0;
-        for (int c = g.d; c < (ext ? KY - 2 : KY); ++c) yr[c] = (ones && c >= KY - 2) || (one && c == KY - 1) ? 0x3f80 : 0;
+        for (int c = g.d; c < KX; ++c) xr[c] = ones && c >= KX - 2 ? 0x3f80 : 0;
+        for (int c = g.d; c < (EXT ? KY - 2 : KY); ++c) yr[c] = (ones && c >= KY - 2) || (one && c == KY - 1) ? 0x3f80 : 0;
     }
 }
 
@@ -317,10 +318,10 @@ __device__ __forceinline__ Rows ckpt_rows_of(const Geo &g, const Place &p, const
     return Rows{(const char *)c + first * dp, dp, c + 3 * rows * dp + first};
 }
 
-template <int KX, int KY, int W>
+template <int KX, int KY, int W, bool EXT = false>
 constexpr size_t stage_bytes()
 {
-    using I = Img<KX, KY>;
+    using I = Img<KX, KY, EXT>;
     const size_t tiles = (size_t)I::TOTAL * 2, stat = (size_t)W * 64 * (KX + 8) * 2;
     return ((tiles > stat ? tiles : stat) + 15) & ~(size_t)15;
 }
@@ -508,7 +509,7 @@ __global__ __launch_bounds__(W * 64, DB == 1 ? 3 : 2) void fwd_kernel(Geo g, Bia
         mylin[qb] = cell_of<ALN>(g, bi, n < g.N ? n : g.N - 1).lin(bi);
     }
     __syncthreads();
-    init_cols<KX, 32 * DB>(g, S, false, false, !SUM, NT);
+    init_cols<KX, 32 * DB>(g, S, false, !SUM, NT);
     f32x16 O[QB][DB];
     float sum[QB], top[QB];
     // First without a running maximum: exp2 of a logit is a normal number far beyond what bounded logits need.  A row whose
@@ -523,7 +524,7 @@ __global__ __launch_bounds__(W * 64, DB == 1 ? 3 : 2) void fwd_kernel(Geo g, Bia
     }
     if (__syncthreads_or(bad)) {
         mv.request(g, bi, pl.win, ks, vs, nullptr, 0);
-        if (SPLIT) init_cols<KX, 32 * DB>(g, S, false, false, !SUM, NT);       // (the first walk's sums went through the tiles)
+        if (SPLIT) init_cols<KX, 32 * DB>(g, S, false, !SUM, NT);       // (the first walk's sums went through the tiles)
         fwd_walk<true, KX, DB, SUM, SRC, ALN, SPLIT, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, mylin, active, mv);
     }
     if (SPLIT && half) return;
@@ -599,9 +600,9 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
             if (lane / (64 / LP) == p) delta = x;
         }
         const bool none = n >= g.N || e == -INFINITY;
-        const uint32_t wl = none ? pack_bf16(-kNoRow, 0.f) : split_bf16(-e * bi.bs), wd = split_bf16(-delta);
+        const uint32_t wd = split_bf16(-delta);
         L = none ? kNoRow : e * kLog2e;
-        if (n < g.N) ext[(int64_t)pl.u * g.N + n] = uint2{wl, wd};
+        if (n < g.N) ext[(int64_t)pl.u * g.N + n] = uint2{__float_as_uint(-L), wd};
         bf16_t *area = S + wave * 64 * (K + 8);
         operands<K, LP, SRC, QB>(hq, g, area, Q, sel, FixScale{bi.qs});
         operands<K, LP, SG, QB>(hd, g, area, D, sel, FixPair<K>{wd});
@@ -615,7 +616,7 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
         mylse[qb] = __shfl(L, (sel + qb) * 32 + col);
     }
     __syncthreads();
-    init_cols<K, K>(g, S, true, false, false, NT);
+    init_cols<K, K>(g, S, true, false, NT);
     f32x16 A[QB][DB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
@@ -721,10 +722,10 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
 {
     constexpr int LP = DB == 1 ? 4 : 8, NT = 64 * W, QB = SPLIT ? 1 : 2, GT = SPLIT ? 64 : NT;      // (GT: the workgroup's stationary tokens)
     constexpr bool CARRY = ALN && !SPLIT;
-    using I = Img<K, K>;
+    using I = Img<K, K, true>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     bf16_t *S = (bf16_t *)smem;
-    int *map = (int *)(smem + stage_bytes<K, K, W>());
+    int *map = (int *)(smem + stage_bytes<K, K, W, true>());
     float *B = (float *)(map + 2 * g.M);
     const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place pl = place_of(g, nblk, NT, map);
@@ -742,7 +743,7 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
         hold<LP, SRC, ALN>(hv, g, bi, pl.win, SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 2) : grid_rows(g, pl, v, g.tstride), n0);
         mv.request(g, bi, pl.win, qs, ds, ex, 0);
         bf16_t *area = S + wave * 64 * (K + 8);
-        operands<K, LP, SRC, QB>(hk, g, area, Kb, sel, FixPair<K>{kOnes});
+        operands<K, LP, SRC, QB>(hk, g, area, Kb, sel, FixScale{1.f});
         operands<K, LP, SRC, QB>(hv, g, area, Vb, sel, FixPair<K>{kOnes});
     }
     int mylin[QB];
@@ -752,7 +753,7 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
         mylin[b] = cell_of<ALN>(g, bi, n < g.N ? n : g.N - 1).lin(bi);
     }
     __syncthreads();
-    init_cols<K, K>(g, S, false, true, false, NT);
+    init_cols<K, K, true>(g, S, false, false, NT);
     f32x16 Ak[QB][DB], Av[QB][DB];
 #pragma unroll
     for (int b = 0; b < QB; ++b)
@@ -786,6 +787,9 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
                     if (!ALN && tile * kTile + qb * 32 >= g.N) break;
                     const Words16<ALN> wd = words_of<ALN>(bi, ch, (const int *)(cur + I::LT), tile, qb, hf);
                     bf16x8 Aq[K / 16], Ad[K / 16], Tq[DB][2], Td[DB][2];
+                    float4 l[4];            // -LSE in base 2 of the lane's 16 queries
+#pragma unroll
+                    for (int a = 0; a < 4; ++a) l[a] = *(const float4 *)((const float *)(cur + I::EX) + qb * 32 + 8 * a + 4 * hf);
                     read_rows<K / 16>(Aq, cur + qb * 32 * I::XS + ako);
                     read_rows<K / 16>(Ad, cur + I::YR + qb * 32 * I::YS + ako);
 #pragma unroll
@@ -806,7 +810,7 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
                         for (int i = 0; i < K / 16; ++i) p = mfma(Ad[i], Vb[b][i], p);
                         uint32_t P[8], G[8];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * bi.c);
+                        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], bi.c, ((const float *)&l[i >> 2])[i & 3]));
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             P[i] = pack_bf16(s[2 * i], s[2 * i + 1]);
@@ -890,7 +894,7 @@ hipError_t launch_pair(const Geo &g, const BwdArgs &a, Ws &ws)
     Bias bi{a.bias};
     plan_scale(g, &bi);
     plan_chunks(g, RIB_BF16, &bi, ALN, SPLIT ? 64 : 64 * W, false, kBiasBytes, 0);
-    const size_t smem = stage_bytes<K, K, W>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.ws * 4;
+    const size_t smem = stage_bytes<K, K, W, true>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.ws * 4;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
     auto kern = dkv_kernel<K, DB, SRC, SG, ALN, SPLIT, W>;
     e = prepare_kernel((const void *)kern, nullptr);

@@ -236,7 +236,8 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
     extern __shared__ __attribute__((aligned(16))) char smem[];
     bf16_t *X = (bf16_t *)smem, *Y = X + IM;                    // q and dO, or k and v
     int *table = (int *)(Y + IM + 32);                          // (transposed reads of the last row may run over its end)
-    double *H = (double *)(table + 64);
+    float *E = (float *)(table + 64);                           // -LSE in base 2
+    double *H = (double *)(E + 64);
     const int count = bi.w2 * bi.w2;
     float *B = (float *)(H + (HIST ? count : 0));
     const int lane = threadIdx.x, col = lane & 31, hf = lane >> 5, nb = (g.N + 31) / 32;
@@ -259,7 +260,7 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
         const Spot sp = spot_of(g, w);
         const int64_t u = (int64_t)w * g.heads + sh.hd;
         Held<LP> hq, hd;
-        uint32_t wl[LP], wd[LP];        // -LSE / scale and -delta of the rows that this lane's group holds, as pairs
+        uint32_t wd[LP];        // -delta of the rows that this lane's group holds, as pairs
         bf16x8 Qb[2][K / 16], Db[2][K / 16];
         // the images of q and dO; rows past the window are zero, and have no probabilities
         auto queries = [&]() {
@@ -269,7 +270,7 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
             for (int p = 0; p < LP; ++p) {
                 const int n = p * (64 / LP) + l;
                 if (j != 0) continue;
-                *(uint32_t *)(X + n * XS + K - 2) = wl[p];
+                *(uint32_t *)(X + n * XS + K - 2) = 0u;         // (there were ones)
                 *(uint32_t *)(Y + n * XS + K - 2) = wd[p];
             }
         };
@@ -314,7 +315,7 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
                 }
 #pragma unroll
                 for (int m = 1; m < LP; m <<= 1) delta += __shfl_xor(delta, m);
-                wl[p] = n >= g.N || e[p] == -INFINITY ? pack_bf16(-kNoRow, 0.f) : split_bf16(-e[p] * bi.bs);
+                if (j == 0) E[n] = n >= g.N || e[p] == -INFINITY ? -kNoRow : -e[p] * kLog2e;
                 wd[p] = n >= g.N ? 0u : split_bf16(-delta);
             }
             queries();
@@ -333,6 +334,7 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
         for (int qb = 0; qb < 2; ++qb) {
             if (qb >= nb) break;
             f32x16 A[DB];
+            const float mylse = E[qb * 32 + col];
 #pragma unroll
             for (int db = 0; db < DB; ++db) A[db] = z;
             for (int kb = 0; kb < nb; ++kb) {
@@ -347,7 +349,7 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
                 for (int i = 0; i < K / 16; ++i) p = mfma(Av[i], Db[qb][i], p);
                 if (kb == nb - 1) mask_rows(s, kb * 32, g.N, hf);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * bi.c) * p[i];
+                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], bi.c, mylse)) * p[i];
                 if (HIST && qb * 32 + col < g.N) add_offsets<false>(H + ch.c0 - mylin[qb], at, s);      // (many lanes at one word are slow)
                 uint32_t P[8];
 #pragma unroll
@@ -385,6 +387,9 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
                 read_rows<K / 16>(Aq, X + qb * 32 * XS + ako);
                 read_rows<K / 16>(Ad, Y + qb * 32 * XS + ako);
                 f32x16 s, p = z;
+                float4 e[4];
+#pragma unroll
+                for (int a = 0; a < 4; ++a) e[a] = *(const float4 *)(E + qb * 32 + 8 * a + 4 * hf);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = B[ch.c0 + mylin[kb] - at(i)];
 #pragma unroll
@@ -393,7 +398,7 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
                 for (int i = 0; i < K / 16; ++i) p = mfma(Ad[i], Vb[kb][i], p);
                 uint32_t P[8], G[8];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * bi.c);
+                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], bi.c, ((const float *)&e[i >> 2])[i & 3]));
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     P[i] = pack_bf16(s[2 * i], s[2 * i + 1]);
@@ -465,7 +470,7 @@ hipError_t launch_bwd_small_one(const Geo &g, const BwdArgs &a, Ws &ws)
     hipError_t e = share_windows(g, &windows, &per, &parts);
     if (e != hipSuccess) return e;
     ws.shares = parts;
-    const size_t smem = ((size_t)2 * 64 * (K + 8) + 32) * 2 + 256 + (size_t)bi.w2 * bi.w2 * (HIST ? 12 : 4);
+    const size_t smem = ((size_t)2 * 64 * (K + 8) + 32) * 2 + 512 + (size_t)bi.w2 * bi.w2 * (HIST ? 12 : 4);
     auto kern = bwd_small_kernel<K, DB, SRC, SG, HIST>;
     e = prepare_kernel((const void *)kern, nullptr);
     if (e != hipSuccess) return e;

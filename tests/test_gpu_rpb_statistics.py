@@ -1,0 +1,61 @@
+"""What a row's softmax is held in: LSE and the sums it comes from, in 32 bits through forward and backward."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2603_06738_amd import binding as rb
+from test_gpu_rpb import DEV, Case, close, np64, repeated, storage
+
+pytestmark = pytest.mark.gpu
+H = 2.0 ** -24          # half a step of fp32
+U = 2.0 ** -8           # and of bf16
+
+# windows of up to 64 tokens, small grids whose waves share 64 stationary tokens, large grids; with strips and without; each source of rows
+KERNELS = [(8, 30, 1), (8, 32, 1), (8, 15, 1), (7, 30, 1), (16, 30, 1), (16, 32, 1), (16, 15, 1), (16, 40, 1), (16, 64, 1), (16, 30, 180), (16, 15, 180), (16, 64, 180),
+           (9, 30, 1), (9, 30, 180), (20, 32, 100), (32, 30, 1)]
+
+
+def uniform(dtype, M, d, copies, value, seed):
+    """A case whose logits are all `value`: q is zero, every bias `value`."""
+    c = Case(dtype, 1, M, M, 1, d, M, 0, seed=seed, scale=1.0)
+    c.q = torch.zeros_like(c.k)
+    c.qkv = torch.cat((c.q, c.k, c.v), -1).contiguous()
+    c.dout = storage(np.random.default_rng(seed).uniform(0.5, 1.5, c.dout.shape), dtype).to(DEV)
+    c.bias.fill_(value)
+    return repeated(c, copies) if copies > 1 else c
+
+
+# (the negative ones: exp of them is zero without a maximum, the positive ones overflow; at the ones beyond 16000 a pair of bf16 parts is 0.04 to 0.09
+# off for windows of 64, 256 and 1024 tokens)
+@pytest.mark.parametrize("M,d,copies", KERNELS)
+@pytest.mark.parametrize("value", [1000.0, -5000.0, 16475.75, 16490.25, 16473.0, -16420.25])
+def test_gradients_of_rows_far_from_zero(M, d, copies, value):
+    """Uniform rows: P = 1 / N whatever the logits' common value.  In fp32 the value rounds a handful of times at its size: bias in the
+    product's unit (2), base 2 (2), LSE (top, its sum with the logarithm, base e and the store: 5), LSE in base 2 (2), the exponent (1);
+    14 H |value| of P holds all of them.  P is then rounded to bf16 (U), as is dv (U).  dbias is a sum of dS, which is not rounded."""
+    c = uniform("bf16", M, d, copies, value, M + d)
+    N = M * M
+    rb.rib_rpb_attn_fwd(c.p, c.q, c.k, c.v, c.bias, c.out, c.lse)
+    rb.rib_rpb_attn_bwd(c.p, c.q, c.k, c.v, c.bias, c.out, c.dout, c.lse, c.dq, c.dk, c.dv, c.dbias, c.ws)
+    t = 14 * H * (abs(value) + 10)
+    do, v, k, out = (np64(x)[0].reshape(N, d) for x in (c.dout, c.v, c.k, c.out))
+    close("lse", c.lse, np.full(c.lse.shape, value + math.log(N)), np.full(c.lse.shape, t + N * H))
+    close("out", c.out[0].reshape(N, d), np.broadcast_to(v.mean(0), (N, d)), np.broadcast_to(U * abs(v.mean(0)) + (2 * U + t + N * H) * abs(v - v.mean(0)).mean(0)
+                                                                                            + N * H * abs(v).mean(0), (N, d)))
+    want = do.mean(0)
+    close("dv", c.dv[0].reshape(N, d), np.broadcast_to(want, (N, d)), np.broadcast_to((1.02 * (t + U) + N * H) * want + U * want, (N, d)))
+    delta = (do * out).sum(1, keepdims=True)
+    dS = (do @ v.T - delta) / N
+    # -delta as two bf16 parts: 2^-16 of it; fp32 sums of d products
+    off = (2.0 ** -16 * abs(delta) + H * (d + 4) * (abs(do) @ abs(v).T + abs(do * out).sum(1, keepdims=True))) / N
+    eS = 1.02 * t * abs(dS) + 1.02 * off
+    close("dq", c.dq[0].reshape(N, d), dS @ k, 1.02 * ((eS + U * abs(dS)) + N * H * abs(dS)) @ abs(k) + U * abs(dS @ k) + 1e-30)
+    assert (c.dk == 0).all()
+    want, tol = np.zeros((2 * M - 1) ** 2), np.zeros((2 * M - 1) ** 2)
+    iy, ix = np.divmod(np.arange(N), M)
+    rel = (iy[:, None] - iy[None, :] + M - 1) * (2 * M - 1) + ix[:, None] - ix[None, :] + M - 1
+    np.add.at(want, rel.reshape(-1), dS.reshape(-1))
+    np.add.at(tol, rel.reshape(-1), (eS + 2 * H * abs(dS)).reshape(-1))
+    close("dbias", c.dbias[0], copies * want, copies * (1.02 * tol + (copies + 40) * H * abs(want)) + 1e-30)
