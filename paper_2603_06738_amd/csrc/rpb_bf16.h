@@ -11,9 +11,9 @@
 // instructions a block, and cost as much accuracy as the rounding of P (2-norm errors of a training step 2.5e-3 so, 3.4e-3 with it; forward 8 %,
 // whole step 5 % slower).
 //
-// The backward's -delta rides in two more columns of dO's rows, as a bf16 pair (high and low part, 2^-17 of it is lost), against
-// ones in V's: the product is then dP - delta.  LSE is an exponent, where such a loss would grow with it: it stays in fp32, and lies beside the
-// rows in LDS where the query is streamed (dkv).  LSE's denominator is
+// LSE and delta stay in fp32: per row beside the lane's own in dq, in LDS beside the streamed rows in dkv, where -delta is the C operand of dP's
+// product.  (As bf16 pairs in two more columns of the rows they cost nothing in 30 columns and a third of a row's in 32, and lose 2^-17 of LSE, which is
+// an exponent.)  LSE's denominator is
 // the sum of P as rounded (a column of ones in V), which O wants, and which moves LSE by 2^-8 at most, in a row of few keys.
 //
 // What bounds it, by counters (16 images of 96 x 96, 32 x 32 windows, 6 heads of 30; forward / dq / dkv 194 / 394 / 315 us): the vector issue is
@@ -31,15 +31,14 @@ namespace bf {
 
 using namespace rows;
 
-constexpr uint32_t kOnes = 0x3f803f80u;
 constexpr float kNoRow = 1e30f;         // in place of LSE where a row has no key: every probability is zero
 
-// LDS image of a tile: X and Y rows, a streamed token's lin() and (EXT) -LSE in base 2.  K: columns of the contracted width.
+// LDS image of a tile: X and Y rows, a streamed token's lin() and (EXT) -LSE in base 2 and -delta.  K: columns of the contracted width.
 template <int KX, int KY, bool EXT = false>
 struct Img {
     static constexpr int XS = KX + 8, YS = KY + 8;
     static constexpr int YR = kTile * XS, LT = YR + kTile * YS, EX = LT + 2 * kTile;
-    static constexpr int STAGE = EX + (EXT ? 2 * kTile : 0);    // bf16 elements
+    static constexpr int STAGE = EX + (EXT ? 4 * kTile : 0);    // bf16 elements
     static constexpr int TOTAL = 2 * STAGE + 32;                // (transposed reads of the last row may run over its end)
 };
 
@@ -121,9 +120,9 @@ template <int LP, int W, int SX, int SY, bool EXT, bool ALN>
 struct Mover {
     static constexpr int NT = 64 * W, P = (kTile * LP + NT - 1) / NT;
     Raw x[P], y[P];
-    uint2 e[EXT ? P : 1];
+    float2 e[EXT ? P : 1];
 
-    __device__ __forceinline__ void request(const Geo &g, const Bias &bi, const Win &win, const Rows &xs, const Rows &ys, const uint2 *ext, int tile)
+    __device__ __forceinline__ void request(const Geo &g, const Bias &bi, const Win &win, const Rows &xs, const Rows &ys, const float2 *ext, int tile)
     {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
@@ -137,8 +136,8 @@ struct Mover {
             if (EXT) e[p] = ext[n];
         }
     }
-    // KX, KY: the images' widths.  ONES: ones in the two last columns of both (dq); EXT: -delta in Y's (dkv).
-    template <int KX, int KY, bool ONES>
+    // KX, KY: the images' widths.
+    template <int KX, int KY>
     __device__ __forceinline__ void commit(const Geo &g, const Bias &bi, bf16_t *S, int tile, float scale)
     {
         using I = Img<KX, KY, EXT>;
@@ -152,28 +151,25 @@ struct Mover {
             Raw a = widen_piece<SX>(x[p]), b = widen_piece<SY>(y[p]);
             if (EXT && scale != 1.f) a = scaled(a, scale);
             if (!in) b.w[0] = b.w[1] = b.w[2] = b.w[3] = 0u;    // (an infinity in the repeated last token must not meet P = 0)
-            if (ONES && SX == kCkpt && piece_col<SX>(j, g.d) == KX - 8) a.w[3] = kOnes;
-            if (ONES && SY == kCkpt && piece_col<SY>(j, g.d) == KY - 8) b.w[3] = kOnes;
             put_piece<SX>(xr, a, j, g.d);
             put_piece<SY>(yr, b, j, g.d);
             if (EXT && j == 0) {
-                ((float *)(S + I::EX))[row] = in ? __uint_as_float(e[p].x) : -kNoRow;
-                *(uint32_t *)(yr + KY - 2) = in ? e[p].y : 0u;
+                ((float *)(S + I::EX))[row] = in ? e[p].x : -kNoRow;
+                ((float *)(S + I::EX))[kTile + row] = in ? e[p].y : 0.f;
             }
             if (!ALN && j == 0) ((int *)(S + I::LT))[row] = cell_of<false>(g, bi, in ? n : g.N - 1).lin(bi);
         }
     }
 };
-// Columns that no commit writes, once for both stages (beside the first commit: what both write is the same).  `ones`: in the last two
-// columns of X and Y; EXT: not those of Y; `one`: in Y's last column.
+// Columns that no commit writes, once for both stages (beside the first commit: what both write is the same).  `one`: a one in Y's last.
 template <int KX, int KY, bool EXT = false>
-__device__ __forceinline__ void init_cols(const Geo &g, bf16_t *S, bool ones, bool one, int nt)
+__device__ __forceinline__ void init_cols(const Geo &g, bf16_t *S, bool one, int nt)
 {
     using I = Img<KX, KY, EXT>;
     for (int e = threadIdx.x; e < 2 * kTile; e += nt) {
         bf16_t *xr = S + (e / kTile) * I::STAGE + (e % kTile) * I::XS, *yr = S + (e / kTile) * I::STAGE + I::YR + (e % kTile) * I::YS;
-        for (int c = g.d; c < KX; ++c) xr[c] = ones && c >= KX - 2 ? 0x3f80 : 0;
-        for (int c = g.d; c < (EXT ? KY - 2 : KY); ++c) yr[c] = (ones && c >= KY - 2) || (one && c == KY - 1) ? 0x3f80 : 0;
+        for (int c = g.d; c < KX; ++c) xr[c] = 0;
+        for (int c = g.d; c < KY; ++c) yr[c] = one && c == KY - 1 ? 0x3f80 : 0;
     }
 }
 
@@ -194,9 +190,9 @@ __device__ __forceinline__ void hold(Held<LP> &h, const Geo &g, const Bias &bi, 
         h.r[p] = get_piece<SRC>(s, SRC == kCkpt ? 0u : pixel(win, c), c.index(g), j, g.d);
     }
 }
-// QB blocks of the rows, from block `sel` on, as B operands, through `area` (64 rows of K + 8 columns, the wave's own).  `fix` may change values and writes further columns.
-template <int K, int LP, int SRC, int QB, class Fix>
-__device__ __forceinline__ void operands(const Held<LP> &h, const Geo &g, bf16_t *area, bf16x8 (&B)[QB][K / 16], int sel, Fix fix)
+// QB blocks of the rows, from block `sel` on, as B operands, times `s`, through `area` (64 rows of K + 8 columns, the wave's own).
+template <int K, int LP, int SRC, int QB>
+__device__ __forceinline__ void operands(const Held<LP> &h, const Geo &g, bf16_t *area, bf16x8 (&B)[QB][K / 16], int sel, float s)
 {
     constexpr int STR = K + 8;
     const int lane = threadIdx.x & 63, l = lane / LP, j = lane % LP;
@@ -206,26 +202,15 @@ __device__ __forceinline__ void operands(const Held<LP> &h, const Geo &g, bf16_t
     }
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int p = 0; p < LP; ++p) put_piece<SRC>(area + (p * (64 / LP) + l) * STR, fix(widen_piece<SRC>(h.r[p])), j, g.d);
-    __builtin_amdgcn_wave_barrier();
-    fix.columns(area, STR);
+    for (int p = 0; p < LP; ++p) {
+        const Raw r = widen_piece<SRC>(h.r[p]);
+        put_piece<SRC>(area + (p * (64 / LP) + l) * STR, s != 1.f ? scaled(r, s) : r, j, g.d);
+    }
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int b = 0; b < QB; ++b) read_rows<K / 16>(B[b], area + ((sel + b) * 32 + (lane & 31)) * STR + 8 * (lane >> 5));
     __builtin_amdgcn_wave_barrier();
 }
-struct FixScale {
-    float s;            // (1: values as they are)
-    __device__ __forceinline__ Raw operator()(const Raw &r) const { return s != 1.f ? scaled(r, s) : r; }
-    __device__ __forceinline__ void columns(bf16_t *, int) const {}
-};
-// The pair `w` of row `lane` in the last two columns.
-template <int K>
-struct FixPair {
-    uint32_t w;
-    __device__ __forceinline__ Raw operator()(const Raw &r) const { return r; }
-    __device__ __forceinline__ void columns(bf16_t *area, int str) const { *(uint32_t *)(area + (threadIdx.x & 63) * str + K - 2) = w; }
-};
 
 // ---- blocks ------------------------------------------------------------------------------------------------------
 
@@ -367,7 +352,7 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
             for (int i = 0; i < 16; ++i) O[qb][db][i] = 0.f;
         sum[qb] = 0.f, top[qb] = MAX ? -INFINITY : 0.f;
     }
-    mv.template commit<KX, KY, false>(g, bi, S, 0, 1.f);
+    mv.template commit<KX, KY>(g, bi, S, 0, 1.f);
     mv.request(g, bi, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
     f32x16 next;            // (CARRY) the bias of block (1, the coming one)
     for (int t0 = 0, t1, end = strip_tiles; t0 < ntiles; t0 = t1) {
@@ -379,7 +364,7 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
         for (int tile = t0; tile < t1; ++tile) {
             const bf16_t *cur = S + (tile & 1) * I::STAGE;
             if (tile + 1 < ntiles) {
-                mv.template commit<KX, KY, false>(g, bi, S + ((tile + 1) & 1) * I::STAGE, tile + 1, 1.f);
+                mv.template commit<KX, KY>(g, bi, S + ((tile + 1) & 1) * I::STAGE, tile + 1, 1.f);
                 mv.request(g, bi, pl.win, ks, vs, nullptr, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
             }
             if (active) {
@@ -500,7 +485,7 @@ __global__ __launch_bounds__(W * 64, DB == 1 ? 3 : 2) void fwd_kernel(Geo g, Bia
         Held<LP> hq;
         hold<LP, SRC, ALN>(hq, g, bi, pl.win, grid_rows(g, pl, q, g.tstride), n0);
         mv.request(g, bi, pl.win, ks, vs, nullptr, 0);
-        operands<KX, LP, SRC, QB>(hq, g, S + wave * 64 * (KX + 8), Q, sel, FixScale{bi.qs});
+        operands<KX, LP, SRC, QB>(hq, g, S + wave * 64 * (KX + 8), Q, sel, bi.qs);
     }
     int mylin[QB];
 #pragma unroll
@@ -509,7 +494,7 @@ __global__ __launch_bounds__(W * 64, DB == 1 ? 3 : 2) void fwd_kernel(Geo g, Bia
         mylin[qb] = cell_of<ALN>(g, bi, n < g.N ? n : g.N - 1).lin(bi);
     }
     __syncthreads();
-    init_cols<KX, 32 * DB>(g, S, false, !SUM, NT);
+    init_cols<KX, 32 * DB>(g, S, !SUM, NT);
     f32x16 O[QB][DB];
     float sum[QB], top[QB];
     // First without a running maximum: exp2 of a logit is a normal number far beyond what bounded logits need.  A row whose
@@ -524,7 +509,7 @@ __global__ __launch_bounds__(W * 64, DB == 1 ? 3 : 2) void fwd_kernel(Geo g, Bia
     }
     if (__syncthreads_or(bad)) {
         mv.request(g, bi, pl.win, ks, vs, nullptr, 0);
-        if (SPLIT) init_cols<KX, 32 * DB>(g, S, false, !SUM, NT);       // (the first walk's sums went through the tiles)
+        if (SPLIT) init_cols<KX, 32 * DB>(g, S, !SUM, NT);       // (the first walk's sums went through the tiles)
         fwd_walk<true, KX, DB, SUM, SRC, ALN, SPLIT, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, mylin, active, mv);
     }
     if (SPLIT && half) return;
@@ -549,7 +534,7 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
                                                        const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
                                                        const uint8_t *__restrict__ ckpt, const bf16_t *__restrict__ out,
                                                        const bf16_t *__restrict__ dout, const float *__restrict__ lse,
-                                                       bf16_t *__restrict__ dq, uint2 *__restrict__ ext, float *__restrict__ part)
+                                                       bf16_t *__restrict__ dq, float2 *__restrict__ ext, float *__restrict__ part)
 {
     constexpr int LP = DB == 1 ? 4 : 8, NT = 64 * W, QB = SPLIT ? 1 : 2, GT = SPLIT ? 64 : NT;      // (GT: the workgroup's stationary tokens)
     constexpr bool CARRY = ALN && !SPLIT;
@@ -573,7 +558,7 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
     const Rows vs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 2) : grid_rows(g, pl, v, g.tstride);
     bf16x8 Q[QB][K / 16], D[QB][K / 16];
     Mover<LP, W, SRC, SRC, false, ALN> mv;
-    float L;            // LSE in base 2 of row `lane`
+    float L, delta = 0.f;       // LSE in base 2 and delta of row `lane`
     {
         Held<LP> hq, hd, ho;
         hold<LP, SG, ALN>(hd, g, bi, pl.win, grid_rows(g, pl, dout, g.C), n0);
@@ -584,7 +569,7 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
         mv.request(g, bi, pl.win, ks, vs, nullptr, 0);
         // delta of the wave's rows: LP lanes share one
         const int j = lane % LP, c = piece_col<SG>(j, g.d);
-        float delta = 0.f;      // of row `lane`: it belongs to pass lane / (64 / LP), lanes (lane % (64 / LP)) * LP ..
+        // (row `lane` belongs to pass lane / (64 / LP), lanes (lane % (64 / LP)) * LP ..)
 #pragma unroll
         for (int p = 0; p < LP; ++p) {
             float s = 0.f;
@@ -600,23 +585,22 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
             if (lane / (64 / LP) == p) delta = x;
         }
         const bool none = n >= g.N || e == -INFINITY;
-        const uint32_t wd = split_bf16(-delta);
         L = none ? kNoRow : e * kLog2e;
-        if (n < g.N) ext[(int64_t)pl.u * g.N + n] = uint2{__float_as_uint(-L), wd};
+        if (n < g.N) ext[(int64_t)pl.u * g.N + n] = float2{-L, -delta};
         bf16_t *area = S + wave * 64 * (K + 8);
-        operands<K, LP, SRC, QB>(hq, g, area, Q, sel, FixScale{bi.qs});
-        operands<K, LP, SG, QB>(hd, g, area, D, sel, FixPair<K>{wd});
+        operands<K, LP, SRC, QB>(hq, g, area, Q, sel, bi.qs);
+        operands<K, LP, SG, QB>(hd, g, area, D, sel, 1.f);
     }
     int mylin[QB];
-    float mylse[QB];
+    float mylse[QB], mydelta[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
         const int n = n0 + (sel + qb) * 32 + col;
         mylin[qb] = cell_of<ALN>(g, bi, n < g.N ? n : g.N - 1).lin(bi);
-        mylse[qb] = __shfl(L, (sel + qb) * 32 + col);
+        mylse[qb] = __shfl(L, (sel + qb) * 32 + col), mydelta[qb] = __shfl(delta, (sel + qb) * 32 + col);
     }
     __syncthreads();
-    init_cols<K, K>(g, S, true, false, NT);
+    init_cols<K, K>(g, S, false, NT);
     f32x16 A[QB][DB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
@@ -627,7 +611,7 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
     const int ntiles = (g.N + kTile - 1) / kTile, strip_tiles = ALN ? bi.strip / kTile : ntiles;
     const int tro = tr_lane_offset<I::XS>(lane), ako = col * I::XS + 8 * hf;
     const f32x16 z = {0};
-    mv.template commit<K, K, true>(g, bi, S, 0, 1.f);
+    mv.template commit<K, K>(g, bi, S, 0, 1.f);
     mv.request(g, bi, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
     f32x16 next, held;      // (CARRY) the bias of block (1, the coming one); dS of block (0, the last one)
     if (CARRY && HIST) held = z;
@@ -642,7 +626,7 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
         for (int tile = t0; tile < t1; ++tile) {
             const bf16_t *cur = S + (tile & 1) * I::STAGE;
             if (tile + 1 < ntiles) {
-                mv.template commit<K, K, true>(g, bi, S + ((tile + 1) & 1) * I::STAGE, tile + 1, 1.f);
+                mv.template commit<K, K>(g, bi, S + ((tile + 1) & 1) * I::STAGE, tile + 1, 1.f);
                 mv.request(g, bi, pl.win, ks, vs, nullptr, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
             }
             if (active) {
@@ -669,7 +653,7 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
                         for (int i = 0; i < K / 16; ++i) p = mfma(Av[i], D[qb][i], p);
                         if (!ALN) mask_rows(s, key0, g.N, hf);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], bi.c, -mylse[qb])) * p[i];
+                        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], bi.c, -mylse[qb])) * (p[i] - mydelta[qb]);
                         if (HIST && CARRY && qb == 1) add_offsets<ALN>(mine - mylin[QB - 1], wd, s + held);
                         else if (HIST && CARRY) held = s;
                         else if (HIST && (ALN || n0 + (sel + qb) * 32 + col < g.N)) add_offsets<ALN>(mine - mylin[qb], wd, s);     // (many lanes at one word are slow)
@@ -718,7 +702,7 @@ template <int K, int DB, int SRC, int SG, bool ALN, bool SPLIT, int W>
 __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk, const bf16_t *__restrict__ q,
                                                         const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
                                                         const uint8_t *__restrict__ ckpt, const bf16_t *__restrict__ dout,
-                                                        const uint2 *__restrict__ ext, bf16_t *__restrict__ dk, bf16_t *__restrict__ dv)
+                                                        const float2 *__restrict__ ext, bf16_t *__restrict__ dk, bf16_t *__restrict__ dv)
 {
     constexpr int LP = DB == 1 ? 4 : 8, NT = 64 * W, QB = SPLIT ? 1 : 2, GT = SPLIT ? 64 : NT;      // (GT: the workgroup's stationary tokens)
     constexpr bool CARRY = ALN && !SPLIT;
@@ -734,7 +718,7 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
     const Span span = span_of<ALN>(g, bi, first, last);
     const bool active = n0 < g.N;
     const Rows qs = SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 0) : grid_rows(g, pl, q, g.tstride), ds = grid_rows(g, pl, dout, g.C);
-    const uint2 *const ex = ext + (int64_t)pl.u * g.N;
+    const float2 *const ex = ext + (int64_t)pl.u * g.N;
     bf16x8 Kb[QB][K / 16], Vb[QB][K / 16];
     Mover<LP, W, SRC, SG, true, ALN> mv;
     {
@@ -743,8 +727,8 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
         hold<LP, SRC, ALN>(hv, g, bi, pl.win, SRC == kCkpt ? ckpt_rows_of(g, pl, ckpt, 2) : grid_rows(g, pl, v, g.tstride), n0);
         mv.request(g, bi, pl.win, qs, ds, ex, 0);
         bf16_t *area = S + wave * 64 * (K + 8);
-        operands<K, LP, SRC, QB>(hk, g, area, Kb, sel, FixScale{1.f});
-        operands<K, LP, SRC, QB>(hv, g, area, Vb, sel, FixPair<K>{kOnes});
+        operands<K, LP, SRC, QB>(hk, g, area, Kb, sel, 1.f);
+        operands<K, LP, SRC, QB>(hv, g, area, Vb, sel, 1.f);
     }
     int mylin[QB];
 #pragma unroll
@@ -753,7 +737,7 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
         mylin[b] = cell_of<ALN>(g, bi, n < g.N ? n : g.N - 1).lin(bi);
     }
     __syncthreads();
-    init_cols<K, K, true>(g, S, false, false, NT);
+    init_cols<K, K, true>(g, S, false, NT);
     f32x16 Ak[QB][DB], Av[QB][DB];
 #pragma unroll
     for (int b = 0; b < QB; ++b)
@@ -764,9 +748,8 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
     const int ntiles = (g.N + kTile - 1) / kTile, strip_tiles = ALN ? bi.strip / kTile : ntiles;
     const int tro = tr_lane_offset<I::XS>(lane), ako = col * I::XS + 8 * hf;
     const float scale = bi.qs;
-    const f32x16 z = {0};
     f32x16 next;            // (CARRY) the bias of block (1, the coming one)
-    mv.template commit<K, K, false>(g, bi, S, 0, scale);
+    mv.template commit<K, K>(g, bi, S, 0, scale);
     mv.request(g, bi, pl.win, qs, ds, ex, ntiles > 1 ? 1 : 0);
     for (int t0 = 0, t1, end = strip_tiles; t0 < ntiles; t0 = t1) {
         t1 = t0 + bi.chunk < end ? t0 + bi.chunk : end;
@@ -777,7 +760,7 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
         for (int tile = t0; tile < t1; ++tile) {
             const bf16_t *cur = S + (tile & 1) * I::STAGE;
             if (tile + 1 < ntiles) {
-                mv.template commit<K, K, false>(g, bi, S + ((tile + 1) & 1) * I::STAGE, tile + 1, scale);
+                mv.template commit<K, K>(g, bi, S + ((tile + 1) & 1) * I::STAGE, tile + 1, scale);
                 mv.request(g, bi, pl.win, qs, ds, ex, tile + 2 < ntiles ? tile + 2 : ntiles - 1);
             }
             if (active) {
@@ -787,9 +770,15 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
                     if (!ALN && tile * kTile + qb * 32 >= g.N) break;
                     const Words16<ALN> wd = words_of<ALN>(bi, ch, (const int *)(cur + I::LT), tile, qb, hf);
                     bf16x8 Aq[K / 16], Ad[K / 16], Tq[DB][2], Td[DB][2];
-                    float4 l[4];            // -LSE in base 2 of the lane's 16 queries
+                    float4 l[4];            // -LSE in base 2 of the lane's 16 queries, and their -delta
+                    f32x16 dl;
 #pragma unroll
-                    for (int a = 0; a < 4; ++a) l[a] = *(const float4 *)((const float *)(cur + I::EX) + qb * 32 + 8 * a + 4 * hf);
+                    for (int a = 0; a < 4; ++a) {
+                        const float *const e = (const float *)(cur + I::EX) + qb * 32 + 8 * a + 4 * hf;
+                        const float4 x = *(const float4 *)(e + kTile);
+                        l[a] = *(const float4 *)e;
+                        dl[4 * a] = x.x, dl[4 * a + 1] = x.y, dl[4 * a + 2] = x.z, dl[4 * a + 3] = x.w;
+                    }
                     read_rows<K / 16>(Aq, cur + qb * 32 * I::XS + ako);
                     read_rows<K / 16>(Ad, cur + I::YR + qb * 32 * I::YS + ako);
 #pragma unroll
@@ -802,7 +791,7 @@ __global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk
 #pragma unroll
                     for (int bx = 0; bx < QB; ++bx) {
                         const int b = QB - 1 - bx;
-                        f32x16 s = CARRY && b == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[b], wd), p = z;
+                        f32x16 s = CARRY && b == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[b], wd), p = dl;
                         if (CARRY && b == 0) next = s;
 #pragma unroll
                         for (int i = 0; i < K / 16; ++i) s = mfma(Aq[i], Kb[b][i], s);
@@ -881,7 +870,7 @@ hipError_t launch_dq_one(const Geo &g, const BwdArgs &a, const Ws &ws)
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * ws.nblk)), dim3(64 * W), smem, a.st, g, bi, ws.nblk, (const bf16_t *)a.q,
                        (const bf16_t *)a.k, (const bf16_t *)a.v, a.ckpt, (const bf16_t *)a.out, (const bf16_t *)a.dout, a.lse,
-                       (bf16_t *)a.dq, (uint2 *)((char *)a.ws + ws.ext), (float *)((char *)a.ws + ws.part));
+                       (bf16_t *)a.dq, (float2 *)((char *)a.ws + ws.ext), (float *)((char *)a.ws + ws.part));
     return hipGetLastError();
 }
 template <int K, int DB, int SRC, int SG, bool ALN, bool SPLIT, int W>
@@ -900,7 +889,7 @@ hipError_t launch_pair(const Geo &g, const BwdArgs &a, Ws &ws)
     e = prepare_kernel((const void *)kern, nullptr);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * ws.nblk)), dim3(64 * W), smem, a.st, g, bi, ws.nblk, (const bf16_t *)a.q,
-                       (const bf16_t *)a.k, (const bf16_t *)a.v, a.ckpt, (const bf16_t *)a.dout, (const uint2 *)((const char *)a.ws + ws.ext),
+                       (const bf16_t *)a.k, (const bf16_t *)a.v, a.ckpt, (const bf16_t *)a.dout, (const float2 *)((const char *)a.ws + ws.ext),
                        (bf16_t *)a.dk, (bf16_t *)a.dv);
     return hipGetLastError();
 }

@@ -6,7 +6,7 @@ namespace rpb {
 namespace bf {
 hipError_t bwd_any(const Geo &g, const BwdArgs &a, Ws &ws)
 {
-    return g.d <= 32 ? launch_bwd<48, 1, kAny>(g, a, ws) : launch_bwd<80, 2, kAny>(g, a, ws);
+    return g.d <= 32 ? launch_bwd<32, 1, kAny>(g, a, ws) : launch_bwd<64, 2, kAny>(g, a, ws);
 }
 }  // namespace bf
 }  // namespace rpb

@@ -34,11 +34,9 @@ hipError_t launch_bwd_bf16(const Geo &g, const BwdArgs &a)
     Ws ws = ws_layout(g, RIB_BF16);
     hipError_t e;
     if (!fast(g, {a.q, a.k, a.v, a.out, a.dout, a.dq, a.dk, a.dv})) e = bwd_any(g, a, ws);
-    else if (g.d <= 30) e = bwd32(g, a, ws);        // two columns beside the head's for -LSE and -delta
-    else if (g.d == 32) e = bwd48(g, a, ws);
-    else if (g.d <= 46) e = bwd48w(g, a, ws);
-    else if (g.d <= 62) e = bwd64(g, a, ws);
-    else e = bwd80(g, a, ws);
+    else if (g.d <= 32) e = bwd32(g, a, ws);
+    else if (g.d <= 48) e = bwd48(g, a, ws);
+    else e = bwd64(g, a, ws);
     if (e != hipSuccess || a.dbias == nullptr) return e;
     return launch_reduce(g, RIB_BF16, ws, (const float *)((const char *)a.ws + ws.part), a.dbias, a.st);
 }

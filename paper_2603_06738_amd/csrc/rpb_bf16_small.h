@@ -66,7 +66,7 @@ __device__ __forceinline__ void hold(Held<LP> &h, const Geo &g, const Rows &s, c
     }
 }
 // (Rows past the window are zero.)
-template <int LP, int SRC, int K, bool ONES>
+template <int LP, int SRC, int K>
 __device__ __forceinline__ void lay(const Held<LP> &h, const Geo &g, bf16_t *image, float scale)
 {
     const int l = threadIdx.x / LP, j = threadIdx.x % LP;
@@ -76,17 +76,15 @@ __device__ __forceinline__ void lay(const Held<LP> &h, const Geo &g, bf16_t *ima
         if (n >= g.N) continue;
         Raw a = widen_piece<SRC>(h.r[p]);
         if (scale != 1.f) a = scaled(a, scale);
-        if (ONES && SRC == kCkpt && piece_col<SRC>(j, g.d) == K - 8) a.w[3] = kOnes;
         put_piece<SRC>(image + n * (K + 8), a, j, g.d);
     }
 }
-// Everything of an image that lay() does not write: padding columns, rows past the window; `pad` in the last two columns.
+// Everything of an image that lay() does not write: padding columns, rows past the window.
 template <int K>
-__device__ __forceinline__ void clear_image(const Geo &g, bf16_t *image, uint32_t pad)
+__device__ __forceinline__ void clear_image(const Geo &g, bf16_t *image)
 {
     const int n = threadIdx.x;
     for (int c = n < g.N ? g.d : 0; c < K; ++c) image[n * (K + 8) + c] = 0;
-    *(uint32_t *)(image + n * (K + 8) + K - 2) = pad;
 }
 
 template <int KX, int DB, bool SUM, int SRC>
@@ -104,8 +102,8 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
     const Share sh = share_of(g, windows, per);
     const Chunk ch = chunk_of<false>(g, bi, 0, 1, Span{0, g.M - 1, 0});
     stage_bias<-1>(g, bi, ch, sh.hd, bi.bs, B, 64);
-    clear_image<KX>(g, X, 0u);
-    clear_image<KY>(g, Y, 0u);
+    clear_image<KX>(g, X);
+    clear_image<KY>(g, Y);
     if (!SUM) Y[lane * I::YS + KY - 1] = 0x3f80;
     table[lane] = lin(g, lane < g.N ? lane : g.N - 1);
     __syncthreads();
@@ -130,11 +128,11 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
     request(sh.w0);
     for (int w = sh.w0; w < sh.w1; ++w) {
         bf16x8 Q[2][KX / 16];
-        lay<LP, SRC, KX, false>(hq, g, X, bi.qs);
+        lay<LP, SRC, KX>(hq, g, X, bi.qs);
 #pragma unroll
         for (int b = 0; b < 2; ++b) read_rows<KX / 16>(Q[b], X + b * 32 * I::XS + ako);
-        lay<LP, SRC, KX, false>(hk, g, X, 1.f);
-        lay<LP, SRC, KY, false>(hv, g, Y, 1.f);
+        lay<LP, SRC, KX>(hk, g, X, 1.f);
+        lay<LP, SRC, KY>(hv, g, Y, 1.f);
         if (w + 1 < sh.w1) request(w + 1);
         f32x16 O[2][DB];
         // `sum`: of P as rounded, which O wants (a column of ones in V has it, where there is one); `exact`: of P before it is rounded, which LSE wants (with few keys
@@ -236,8 +234,8 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
     extern __shared__ __attribute__((aligned(16))) char smem[];
     bf16_t *X = (bf16_t *)smem, *Y = X + IM;                    // q and dO, or k and v
     int *table = (int *)(Y + IM + 32);                          // (transposed reads of the last row may run over its end)
-    float *E = (float *)(table + 64);                           // -LSE in base 2
-    double *H = (double *)(E + 64);
+    float *E = (float *)(table + 64);                           // -LSE in base 2, then -delta
+    double *H = (double *)(E + 128);
     const int count = bi.w2 * bi.w2;
     float *B = (float *)(H + (HIST ? count : 0));
     const int lane = threadIdx.x, col = lane & 31, hf = lane >> 5, nb = (g.N + 31) / 32;
@@ -247,8 +245,8 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
     stage_bias<-1>(g, bi, ch, sh.hd, bi.bs, B, 64);
     if (HIST)
         for (int e = lane; e < count; e += 64) H[e] = 0.;
-    clear_image<K>(g, X, 0u);
-    clear_image<K>(g, Y, 0u);
+    clear_image<K>(g, X);
+    clear_image<K>(g, Y);
     table[lane] = lin(g, lane < g.N ? lane : g.N - 1);
     __syncthreads();
     int mylin[2];
@@ -260,19 +258,11 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
         const Spot sp = spot_of(g, w);
         const int64_t u = (int64_t)w * g.heads + sh.hd;
         Held<LP> hq, hd;
-        uint32_t wd[LP];        // -delta of the rows that this lane's group holds, as pairs
         bf16x8 Qb[2][K / 16], Db[2][K / 16];
         // the images of q and dO; rows past the window are zero, and have no probabilities
         auto queries = [&]() {
-            lay<LP, SRC, K, false>(hq, g, X, bi.qs);
-            lay<LP, SG, K, false>(hd, g, Y, 1.f);
-#pragma unroll
-            for (int p = 0; p < LP; ++p) {
-                const int n = p * (64 / LP) + l;
-                if (j != 0) continue;
-                *(uint32_t *)(X + n * XS + K - 2) = 0u;         // (there were ones)
-                *(uint32_t *)(Y + n * XS + K - 2) = wd[p];
-            }
+            lay<LP, SRC, K>(hq, g, X, bi.qs);
+            lay<LP, SG, K>(hd, g, Y, 1.f);
         };
         {
             uint32_t t[LP];
@@ -315,8 +305,7 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
                 }
 #pragma unroll
                 for (int m = 1; m < LP; m <<= 1) delta += __shfl_xor(delta, m);
-                if (j == 0) E[n] = n >= g.N || e[p] == -INFINITY ? -kNoRow : -e[p] * kLog2e;
-                wd[p] = n >= g.N ? 0u : split_bf16(-delta);
+                if (j == 0) E[n] = n >= g.N || e[p] == -INFINITY ? -kNoRow : -e[p] * kLog2e, E[64 + n] = n >= g.N ? 0.f : -delta;
             }
             queries();
 #pragma unroll
@@ -324,17 +313,15 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
                 read_rows<K / 16>(Qb[b], X + b * 32 * XS + ako);
                 read_rows<K / 16>(Db[b], Y + b * 32 * XS + ako);
             }
-            lay<LP, SRC, K, true>(hk, g, X, 1.f);
-            lay<LP, SRC, K, true>(hv, g, Y, 1.f);
-            *(uint32_t *)(X + lane * XS + K - 2) = kOnes;
-            *(uint32_t *)(Y + lane * XS + K - 2) = kOnes;
+            lay<LP, SRC, K>(hk, g, X, 1.f);
+            lay<LP, SRC, K>(hv, g, Y, 1.f);
         }
         // dq and the offsets' sums: a lane owns a query
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb) {
             if (qb >= nb) break;
             f32x16 A[DB];
-            const float mylse = E[qb * 32 + col];
+            const float mylse = E[qb * 32 + col], mydelta = E[64 + qb * 32 + col];
 #pragma unroll
             for (int db = 0; db < DB; ++db) A[db] = z;
             for (int kb = 0; kb < nb; ++kb) {
@@ -349,7 +336,7 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
                 for (int i = 0; i < K / 16; ++i) p = mfma(Av[i], Db[qb][i], p);
                 if (kb == nb - 1) mask_rows(s, kb * 32, g.N, hf);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], bi.c, mylse)) * p[i];
+                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], bi.c, mylse)) * (p[i] + mydelta);
                 if (HIST && qb * 32 + col < g.N) add_offsets<false>(H + ch.c0 - mylin[qb], at, s);      // (many lanes at one word are slow)
                 uint32_t P[8];
 #pragma unroll
@@ -386,10 +373,14 @@ __global__ __launch_bounds__(64, 2) void bwd_small_kernel(Geo g, Bias bi, int wi
                 bf16x8 Aq[K / 16], Ad[K / 16];
                 read_rows<K / 16>(Aq, X + qb * 32 * XS + ako);
                 read_rows<K / 16>(Ad, Y + qb * 32 * XS + ako);
-                f32x16 s, p = z;
+                f32x16 s, p;
                 float4 e[4];
 #pragma unroll
-                for (int a = 0; a < 4; ++a) e[a] = *(const float4 *)(E + qb * 32 + 8 * a + 4 * hf);
+                for (int a = 0; a < 4; ++a) {
+                    const float4 x = *(const float4 *)(E + 64 + qb * 32 + 8 * a + 4 * hf);
+                    e[a] = *(const float4 *)(E + qb * 32 + 8 * a + 4 * hf);
+                    p[4 * a] = x.x, p[4 * a + 1] = x.y, p[4 * a + 2] = x.z, p[4 * a + 3] = x.w;
+                }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = B[ch.c0 + mylin[kb] - at(i)];
 #pragma unroll
@@ -470,7 +461,7 @@ hipError_t launch_bwd_small_one(const Geo &g, const BwdArgs &a, Ws &ws)
     hipError_t e = share_windows(g, &windows, &per, &parts);
     if (e != hipSuccess) return e;
     ws.shares = parts;
-    const size_t smem = ((size_t)2 * 64 * (K + 8) + 32) * 2 + 512 + (size_t)bi.w2 * bi.w2 * (HIST ? 12 : 4);
+    const size_t smem = ((size_t)2 * 64 * (K + 8) + 32) * 2 + 768 + (size_t)bi.w2 * bi.w2 * (HIST ? 12 : 4);
     auto kern = bwd_small_kernel<K, DB, SRC, SG, HIST>;
     e = prepare_kernel((const void *)kern, nullptr);
     if (e != hipSuccess) return e;
@@ -531,9 +522,7 @@ hipError_t launch_bwd(const Geo &g, const BwdArgs &a, Ws &ws)
 // One translation unit a width.
 hipError_t bwd32(const Geo &, const BwdArgs &, Ws &);
 hipError_t bwd48(const Geo &, const BwdArgs &, Ws &);
-hipError_t bwd48w(const Geo &, const BwdArgs &, Ws &);
 hipError_t bwd64(const Geo &, const BwdArgs &, Ws &);
-hipError_t bwd80(const Geo &, const BwdArgs &, Ws &);
 hipError_t bwd_any(const Geo &, const BwdArgs &, Ws &);
 
 }  // namespace bf

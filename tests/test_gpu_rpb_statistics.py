@@ -59,3 +59,27 @@ def test_gradients_of_rows_far_from_zero(M, d, copies, value):
     np.add.at(want, rel.reshape(-1), dS.reshape(-1))
     np.add.at(tol, rel.reshape(-1), (eS + 2 * H * abs(dS)).reshape(-1))
     close("dbias", c.dbias[0], copies * want, copies * (1.02 * tol + (copies + 40) * H * abs(want)) + 1e-30)
+
+
+@pytest.mark.parametrize("M,d,copies", [k for k in KERNELS if k[1] in (15, 30)] + [(8, 8, 1), (7, 8, 1), (16, 8, 1), (16, 8, 180), (9, 9, 1), (9, 8, 180), (24, 8, 1)])
+def test_gradients_that_vanish(M, d, copies):
+    """Every token sees itself alone: dP = delta, so dS is zero but for the fp32 sums of d products, whatever the size of delta (positive
+    dO and v of 1 to 2: the sum of their magnitudes is delta).  A sum of d products rounds at most d times at its size, H each, in two orders; LSE
+    and P are 1 to within 1.02."""
+    c = Case("bf16", 1, M, M, 1, d, M, 0, seed=M)
+    rng = np.random.default_rng(d)
+    c.v, c.dout = (storage(rng.uniform(1, 2, c.v.shape), "bf16").to(DEV) for _ in range(2))
+    c.qkv = torch.cat((c.q, c.k, c.v), -1).contiguous()
+    c.bias.fill_(-math.inf)
+    c.bias[:, (2 * M - 1) ** 2 // 2] = 0.0
+    if copies > 1:
+        c = repeated(c, copies)
+    rb.rib_rpb_attn_fwd(c.p, c.q, c.k, c.v, c.bias, c.out, c.lse)
+    c.out.copy_(c.v)                # (what softmax of one key gives)
+    rb.rib_rpb_attn_bwd(c.p, c.q, c.k, c.v, c.bias, c.out, c.dout, c.lse, c.dq, c.dk, c.dv, c.dbias, c.ws)
+    q, k, v, do = (np64(x)[0] for x in (c.q, c.k, c.v, c.dout))
+    off = 1.02 * 2 * d * H * (do * v).sum(-1, keepdims=True)
+    assert (abs(np64(c.dq)[0]) <= 1.02 * c.scale * off * abs(k)).all() and (abs(np64(c.dk)[0]) <= 1.02 * c.scale * off * abs(q)).all()
+    centre = (2 * M - 1) ** 2 // 2
+    assert abs(float(c.dbias[0, centre])) <= 1.02 * copies * off.sum()
+    assert (c.dbias[0, :centre] == 0).all() and (c.dbias[0, centre + 1:] == 0).all()
