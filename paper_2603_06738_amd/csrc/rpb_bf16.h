@@ -529,8 +529,11 @@ __global__ __launch_bounds__(W * 64, DB == 1 ? 3 : 2) void fwd_kernel(Geo g, Bia
 
 // ---- backward: dq and the bias's gradient -------------------------------------------------------------------------
 
+// Two blocks of channels are more than 256 registers hold.  One wave a SIMD has 512 and spills nothing; whether that beats two that spill is measured (8 images
+// of 96 x 96, 4 heads; us, two waves / one): dkv, 32 x 32 windows of 64 channels 1145 / 282, 24 x 24 of 48 673 / 182, 12 x 12 of 64 320 / 117: one
+// throughout; dq, in strips, 64 columns 437 / 323, 48 columns 201 / 226, without strips 12 x 12 of 64 135 / 143, 20 x 20 of 40 170 / 246: one in the first.
 template <int K, int DB, int SRC, int SG, bool ALN, bool SPLIT, int W, bool HIST>
-__global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk, const bf16_t *__restrict__ q,
+__global__ __launch_bounds__(W * 64, DB == 2 && K == 64 && ALN && !SPLIT ? 1 : 2) void dq_kernel(Geo g, Bias bi, int nblk, const bf16_t *__restrict__ q,
                                                        const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
                                                        const uint8_t *__restrict__ ckpt, const bf16_t *__restrict__ out,
                                                        const bf16_t *__restrict__ dout, const float *__restrict__ lse,
@@ -611,6 +614,17 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
     const int ntiles = (g.N + kTile - 1) / kTile, strip_tiles = ALN ? bi.strip / kTile : ntiles;
     const int tro = tr_lane_offset<I::XS>(lane), ako = col * I::XS + 8 * hf;
     const f32x16 z = {0};
+    // -delta as the C operand of dP's product, held (the compiler would make it again for every product), where there are registers for it: up to 32
+    // channels (dq of 32 x 32 windows, 6 heads of 30: 413 us with the subtraction, 386 so)
+    constexpr bool MINUS = DB == 1;
+    f32x16 minus[QB];
+    if (MINUS)
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) minus[qb][i] = -mydelta[qb];
+            asm volatile("" : "+v"(minus[qb]));
+        }
     mv.template commit<K, K>(g, bi, S, 0, 1.f);
     mv.request(g, bi, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
     f32x16 next, held;      // (CARRY) the bias of block (1, the coming one); dS of block (0, the last one)
@@ -645,7 +659,7 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
 #pragma unroll
                     for (int qx = 0; qx < QB; ++qx) {
                         const int qb = QB - 1 - qx;
-                        f32x16 s = CARRY && qb == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[qb], wd), p = z;
+                        f32x16 s = CARRY && qb == 1 ? next : bias_block<ALN>(B + ch.c0 - mylin[qb], wd), p = MINUS ? minus[qb] : z;
                         if (CARRY && qb == 0) next = s;
 #pragma unroll
                         for (int i = 0; i < K / 16; ++i) s = mfma(Ak[i], Q[qb][i], s);
@@ -653,7 +667,7 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
                         for (int i = 0; i < K / 16; ++i) p = mfma(Av[i], D[qb][i], p);
                         if (!ALN) mask_rows(s, key0, g.N, hf);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], bi.c, -mylse[qb])) * (p[i] - mydelta[qb]);
+                        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], bi.c, -mylse[qb])) * (MINUS ? p[i] : p[i] - mydelta[qb]);
                         if (HIST && CARRY && qb == 1) add_offsets<ALN>(mine - mylin[QB - 1], wd, s + held);
                         else if (HIST && CARRY) held = s;
                         else if (HIST && (ALN || n0 + (sel + qb) * 32 + col < g.N)) add_offsets<ALN>(mine - mylin[qb], wd, s);     // (many lanes at one word are slow)
@@ -699,7 +713,7 @@ __global__ __launch_bounds__(W * 64, 2) void dq_kernel(Geo g, Bias bi, int nblk,
 // ---- backward: dk, dv --------------------------------------------------------------------------------------------
 
 template <int K, int DB, int SRC, int SG, bool ALN, bool SPLIT, int W>
-__global__ __launch_bounds__(W * 64, 2) void dkv_kernel(Geo g, Bias bi, int nblk, const bf16_t *__restrict__ q,
+__global__ __launch_bounds__(W * 64, DB == 1 || SPLIT ? 2 : 1) void dkv_kernel(Geo g, Bias bi, int nblk, const bf16_t *__restrict__ q,
                                                         const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
                                                         const uint8_t *__restrict__ ckpt, const bf16_t *__restrict__ dout,
                                                         const float2 *__restrict__ ext, bf16_t *__restrict__ dk, bf16_t *__restrict__ dv)
