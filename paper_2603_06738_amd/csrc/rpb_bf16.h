@@ -13,8 +13,7 @@
 //
 // LSE and delta stay in fp32: per row beside the lane's own in dq, in LDS beside the streamed rows in dkv, where -delta is the C operand of dP's
 // product.  (As bf16 pairs in two more columns of the rows they cost nothing in 30 columns and a third of a row's in 32, and lose 2^-17 of LSE, which is
-// an exponent.)  LSE's denominator is
-// the sum of P as rounded (a column of ones in V), which O wants, and which moves LSE by 2^-8 at most, in a row of few keys.
+// an exponent.)
 //
 // What bounds it, by counters (16 images of 96 x 96, 32 x 32 windows, 6 heads of 30; forward / dq / dkv 194 / 394 / 315 us): the vector issue is
 // busy 60 % of the time and the matrix pipe 29 / 20 / 35 %, and the two hardly overlap.  A block of the forward has 60 vector instructions,
@@ -332,10 +331,22 @@ __device__ __forceinline__ void join(f32x16 (&v)[DB], float *lds, bool odd)
 
 // ---- forward -----------------------------------------------------------------------------------------------------
 
+// Two denominators of a row.  O's weights are P as rounded, so O is divided by the sum of those: a row of one key gives its v.  LSE wants P before it is rounded (with
+// few keys the other sum would move it by up to 2^-8).  The first is a column of ones in V where V's block has one to spare, else (SUM)
+// one instruction for two values of P; the second 16 additions a block, made only where LSE is asked for (forward of 32 x 32 windows, 6 heads of 30,
+// 16 images: 191 us without, 210 with).
+__device__ __forceinline__ float add_pair(float sum, uint32_t pair)
+{
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3f803f80u), sum, false);
+}
+struct Sums {
+    float rounded, exact;
+};
+
 // One walk over the keys; `mv` holds the first tile.  MAX: with the running maximum of every row.
-template <bool MAX, int KX, int DB, bool SUM, int SRC, bool ALN, bool SPLIT, int W>
+template <bool MAX, int KX, int DB, bool SUM, bool LSE, int SRC, bool ALN, bool SPLIT, int W>
 __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Place &pl, const Rows &ks, const Rows &vs, bf16_t *S, float *B,
-                                         const bf16x8 (&Q)[SPLIT ? 1 : 2][KX / 16], f32x16 (&O)[SPLIT ? 1 : 2][DB], float (&sum)[SPLIT ? 1 : 2], float (&top)[SPLIT ? 1 : 2], const Span &span,
+                                         const bf16x8 (&Q)[SPLIT ? 1 : 2][KX / 16], f32x16 (&O)[SPLIT ? 1 : 2][DB], Sums (&sum)[SPLIT ? 1 : 2], float (&top)[SPLIT ? 1 : 2], const Span &span,
                                          const int (&mylin)[SPLIT ? 1 : 2], bool active, Mover<KX <= 32 ? 4 : 8, W, SRC, SRC, false, ALN> &mv)
 {
     constexpr int KY = 32 * DB, NT = 64 * W, QB = SPLIT ? 1 : 2;
@@ -350,7 +361,7 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
         for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int i = 0; i < 16; ++i) O[qb][db][i] = 0.f;
-        sum[qb] = 0.f, top[qb] = MAX ? -INFINITY : 0.f;
+        sum[qb] = Sums{0.f, 0.f}, top[qb] = MAX ? -INFINITY : 0.f;
     }
     mv.template commit<KX, KY>(g, bi, S, 0, 1.f);
     mv.request(g, bi, pl.win, ks, vs, nullptr, ntiles > 1 ? 1 : 0);
@@ -397,7 +408,7 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
                             // (a row of minus infinities so far: any finite stabiliser does)
                             const float ms = m == -INFINITY ? 0.f : m, alpha = __builtin_amdgcn_exp2f(top[qb] - ms);
                             top[qb] = m;
-                            sum[qb] *= alpha;
+                            sum[qb].rounded *= alpha, sum[qb].exact *= alpha;
 #pragma unroll
                             for (int i = 0; i < 16; ++i) s[i] -= ms;
 #pragma unroll
@@ -410,11 +421,17 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
                         for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]);
 #pragma unroll
                         for (int i = 0; i < 8; ++i) P[i] = pack_bf16(s[2 * i], s[2 * i + 1]);
-                        if (SUM) {
+                        if (LSE) {
                             float a = 0.f, b = 0.f;
 #pragma unroll
                             for (int i = 0; i < 8; ++i) a += s[2 * i], b += s[2 * i + 1];
-                            sum[qb] += a + b;
+                            sum[qb].exact += a + b;
+                        }
+                        if (SUM) {
+                            float a = 0.f, b = 0.f;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) a = add_pair(a, P[2 * i]), b = add_pair(b, P[2 * i + 1]);
+                            sum[qb].rounded += a + b;
                         }
 #pragma unroll
                         for (int db = 0; db < DB; ++db) {
@@ -430,13 +447,13 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
     }
     if constexpr (SPLIT) {
         // the two halves' sums; with maxima of their own they are first brought to the larger one
-        float *const part = (float *)S + (threadIdx.x >> 7) * (16 * DB + 2) * 64 + lane;
+        float *const part = (float *)S + (threadIdx.x >> 7) * (16 * DB + 3) * 64 + lane;
         if (half) {
-            part[0] = top[0], part[64] = sum[0];
+            part[0] = top[0], part[64] = sum[0].rounded, part[128] = sum[0].exact;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) part[(2 + 16 * db + i) * 64] = O[0][db][i];
+                for (int i = 0; i < 16; ++i) part[(3 + 16 * db + i) * 64] = O[0][db][i];
         }
         __syncthreads();
         if (!half) {
@@ -446,23 +463,24 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
                 a = __builtin_amdgcn_exp2f(top[0] - ms), b = __builtin_amdgcn_exp2f(part[0] - ms);
                 top[0] = m;
             }
-            sum[0] = sum[0] * a + part[64] * b;
+            sum[0].rounded = sum[0].rounded * a + part[64] * b, sum[0].exact = sum[0].exact * a + part[128] * b;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) O[0][db][i] = O[0][db][i] * a + part[(2 + 16 * db + i) * 64] * b;
+                for (int i = 0; i < 16; ++i) O[0][db][i] = O[0][db][i] * a + part[(3 + 16 * db + i) * 64] * b;
         }
         __syncthreads();
     }
-    // the denominator: the last row of O^T is register 15 of the upper lane half
+    // (the column of ones: the last row of O^T is register 15 of the upper lane half)
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-        const float mine = SUM ? sum[qb] : O[qb][DB - 1][15], other = __shfl_xor(mine, 32);
-        sum[qb] = SUM ? mine + other : hf ? mine : other;
+        const float mine = SUM ? sum[qb].rounded : O[qb][DB - 1][15], other = __shfl_xor(mine, 32);
+        sum[qb].rounded = SUM ? mine + other : hf ? mine : other;
+        if (LSE) sum[qb].exact += __shfl_xor(sum[qb].exact, 32);
     }
 }
 
-template <int KX, int DB, bool SUM, int SRC, bool ALN, bool SPLIT, int W>
+template <int KX, int DB, bool SUM, bool LSE, int SRC, bool ALN, bool SPLIT, int W>
 __global__ __launch_bounds__(W * 64, DB == 1 ? 3 : 2) void fwd_kernel(Geo g, Bias bi, int nblk, int force_max, const bf16_t *__restrict__ q,
                                                         const bf16_t *__restrict__ k, const bf16_t *__restrict__ v,
                                                         bf16_t *__restrict__ out, float *__restrict__ lse)
@@ -496,21 +514,22 @@ __global__ __launch_bounds__(W * 64, DB == 1 ? 3 : 2) void fwd_kernel(Geo g, Bia
     __syncthreads();
     init_cols<KX, 32 * DB>(g, S, !SUM, NT);
     f32x16 O[QB][DB];
-    float sum[QB], top[QB];
+    Sums sum[QB];
+    float top[QB];
     // First without a running maximum: exp2 of a logit is a normal number far beyond what bounded logits need.  A row whose
     // denominator leaves [2^-60, 2^60], and not for want of keys, sends the workgroup on a second walk, with one.
     bool bad = true;
     if (!force_max) {
-        fwd_walk<false, KX, DB, SUM, SRC, ALN, SPLIT, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, mylin, active, mv);
+        fwd_walk<false, KX, DB, SUM, LSE, SRC, ALN, SPLIT, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, mylin, active, mv);
         bad = false;
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb)
-            if (active && !(SPLIT && half) && bad_rows(g, bi, pl.hd, n0 + (sel + qb) * 32 + col < g.N ? cell_of<ALN>(g, bi, n0 + (sel + qb) * 32 + col).index(g) : g.N, sum[qb])) bad = true;
+            if (active && !(SPLIT && half) && bad_rows(g, bi, pl.hd, n0 + (sel + qb) * 32 + col < g.N ? cell_of<ALN>(g, bi, n0 + (sel + qb) * 32 + col).index(g) : g.N, sum[qb].rounded)) bad = true;
     }
     if (__syncthreads_or(bad)) {
         mv.request(g, bi, pl.win, ks, vs, nullptr, 0);
         if (SPLIT) init_cols<KX, 32 * DB>(g, S, !SUM, NT);       // (the first walk's sums went through the tiles)
-        fwd_walk<true, KX, DB, SUM, SRC, ALN, SPLIT, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, mylin, active, mv);
+        fwd_walk<true, KX, DB, SUM, LSE, SRC, ALN, SPLIT, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, mylin, active, mv);
     }
     if (SPLIT && half) return;
 #pragma unroll
@@ -518,9 +537,10 @@ __global__ __launch_bounds__(W * 64, DB == 1 ? 3 : 2) void fwd_kernel(Geo g, Bia
         const int n = n0 + (sel + qb) * 32 + col;
         if (n >= g.N) continue;
         const Cell c = cell_of<ALN>(g, bi, n);
-        const float inv = sum[qb] == 0.f ? 0.f : 1.f / sum[qb];         // (a row without a key: zeros)
-        if (lse != nullptr && hf == 0)
-            lse[(int64_t)pl.u * g.N + c.index(g)] = sum[qb] == 0.f ? -INFINITY : (top[qb] + __builtin_amdgcn_logf(sum[qb])) * kLn2;
+        const bool none = sum[qb].rounded == 0.f;
+        const float inv = none ? 0.f : 1.f / sum[qb].rounded;           // (a row without a key: zeros)
+        // (asked of the pointer, which is null without LSE: where `top` goes unused the compiler spills up to 181 registers)
+        if (lse != nullptr && hf == 0) lse[(int64_t)pl.u * g.N + c.index(g)] = none ? -INFINITY : (top[qb] + __builtin_amdgcn_logf(LSE ? sum[qb].exact : sum[qb].rounded)) * kLn2;
         bf16_t *row = out + (pl.img + pixel(pl.win, c)) * g.C + pl.hd * g.d;
 #pragma unroll
         for (int db = 0; db < DB; ++db) store_row<SRC>(row, O[qb][db], db, g.d, hf, inv);
@@ -855,8 +875,8 @@ __global__ __launch_bounds__(W * 64, DB == 1 || SPLIT ? 2 : 1) void dkv_kernel(G
 
 constexpr size_t kBiasBytes = 36 * 1024, kHistBytes = 9 * 1024;
 
-template <int KX, int DB, bool SUM, int SRC, bool ALN, bool SPLIT, int W>
-hipError_t launch_fwd_one(const Geo &g, const FwdArgs &a)
+template <int KX, int DB, bool SUM, bool LSE, int SRC, bool ALN, bool SPLIT, int W>
+hipError_t launch_fwd_lse(const Geo &g, const FwdArgs &a)
 {
     Bias bi{a.bias};
     plan_scale(g, &bi);
@@ -864,12 +884,17 @@ hipError_t launch_fwd_one(const Geo &g, const FwdArgs &a)
     const int nblk = (g.N + (SPLIT ? 64 : 64 * W) - 1) / (SPLIT ? 64 : 64 * W);
     const size_t smem = stage_bytes<KX, 32 * DB, W>() + 8 * (size_t)g.M + (size_t)bi.rows * bi.ws * 4;
     if (smem > (size_t)kMaxDynLds) return hipErrorInvalidValue;
-    auto kern = fwd_kernel<KX, DB, SUM, SRC, ALN, SPLIT, W>;
+    auto kern = fwd_kernel<KX, DB, SUM, LSE, SRC, ALN, SPLIT, W>;
     const hipError_t e = prepare_kernel((const void *)kern, nullptr);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)(g.units * nblk)), dim3(64 * W), smem, a.st, g, bi, nblk, a.force_max, (const bf16_t *)a.q,
                        (const bf16_t *)a.k, (const bf16_t *)a.v, (bf16_t *)a.out, a.lse);
     return hipGetLastError();
+}
+template <int KX, int DB, bool SUM, int SRC, bool ALN, bool SPLIT, int W>
+hipError_t launch_fwd_one(const Geo &g, const FwdArgs &a)
+{
+    return a.lse != nullptr ? launch_fwd_lse<KX, DB, SUM, true, SRC, ALN, SPLIT, W>(g, a) : launch_fwd_lse<KX, DB, SUM, false, SRC, ALN, SPLIT, W>(g, a);
 }
 template <int K, int DB, int SRC, int SG, bool ALN, bool SPLIT, int W, bool HIST>
 hipError_t launch_dq_one(const Geo &g, const BwdArgs &a, const Ws &ws)

@@ -87,7 +87,7 @@ __device__ __forceinline__ void clear_image(const Geo &g, bf16_t *image)
     for (int c = n < g.N ? g.d : 0; c < K; ++c) image[n * (K + 8) + c] = 0;
 }
 
-template <int KX, int DB, bool SUM, int SRC>
+template <int KX, int DB, bool SUM, bool LSE, int SRC>
 __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, Bias bi, int windows, int per, int force_max, const bf16_t *__restrict__ q,
                                                           const bf16_t *__restrict__ k, const bf16_t *__restrict__ v, bf16_t *__restrict__ out,
                                                           float *__restrict__ lse)
@@ -135,9 +135,8 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
         lay<LP, SRC, KY>(hv, g, Y, 1.f);
         if (w + 1 < sh.w1) request(w + 1);
         f32x16 O[2][DB];
-        // `sum`: of P as rounded, which O wants (a column of ones in V has it, where there is one); `exact`: of P before it is rounded, which LSE wants (with few keys
-        // the other would move it by up to 2^-8)
-        float sum[2] = {0.f, 0.f}, top[2] = {0.f, 0.f}, exact[2] = {0.f, 0.f};
+        Sums sum[2];
+        float top[2] = {0.f, 0.f};
         // all keys of a block of queries at once: scores first, so that their maximum is at hand where it is wanted
         auto walk = [&](bool max) {
 #pragma unroll
@@ -167,7 +166,7 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
                     m = fmaxf(m, __shfl_xor(m, 32));
                     top[qb] = m == -INFINITY ? 0.f : m;         // (a row without a key: any finite stabiliser does)
                 }
-                exact[qb] = sum[qb] = 0.f;
+                sum[qb] = Sums{0.f, 0.f};
 #pragma unroll
                 for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -180,15 +179,17 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
                     for (int i = 0; i < 16; ++i) s[kb][i] = __builtin_amdgcn_exp2f(s[kb][i] - top[qb]);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) P[i] = pack_bf16(s[kb][2 * i], s[kb][2 * i + 1]);
-                    float a = 0.f, b = 0.f;
+                    if (LSE) {
+                        float a = 0.f, b = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) a += s[kb][2 * i], b += s[kb][2 * i + 1];
-                    exact[qb] += a + b;
+                        for (int i = 0; i < 8; ++i) a += s[kb][2 * i], b += s[kb][2 * i + 1];
+                        sum[qb].exact += a + b;
+                    }
                     if (SUM) {
-                        float r = 0.f;
+                        float a = 0.f, b = 0.f;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) r += lo_bf16(P[i]) + hi_bf16(P[i]);
-                        sum[qb] += r;
+                        for (int i = 0; i < 4; ++i) a = add_pair(a, P[2 * i]), b = add_pair(b, P[2 * i + 1]);
+                        sum[qb].rounded += a + b;
                     }
 #pragma unroll
                     for (int db = 0; db < DB; ++db) {
@@ -196,9 +197,9 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
                         O[qb][db] = mfma(read_tr<I::YS>(Y + (kb * 32 + 16) * I::YS, tro, 32 * db), as_bf16x8(P[4], P[5], P[6], P[7]), O[qb][db]);
                     }
                 }
-                exact[qb] += __shfl_xor(exact[qb], 32);
-                const float mine = SUM ? sum[qb] : O[qb][DB - 1][15], other = __shfl_xor(mine, 32);
-                sum[qb] = SUM ? mine + other : hf ? mine : other;
+                if (LSE) sum[qb].exact += __shfl_xor(sum[qb].exact, 32);
+                const float mine = SUM ? sum[qb].rounded : O[qb][DB - 1][15], other = __shfl_xor(mine, 32);
+                sum[qb].rounded = SUM ? mine + other : hf ? mine : other;
             }
         };
         bool bad = force_max != 0;
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
             walk(false);
 #pragma unroll
             for (int qb = 0; qb < 2; ++qb)
-                if (qb < nb && bad_rows(g, bi, sh.hd, qb * 32 + col, qb * 32 + col < g.N ? sum[qb] : 1.f)) bad = true;
+                if (qb < nb && bad_rows(g, bi, sh.hd, qb * 32 + col, qb * 32 + col < g.N ? sum[qb].rounded : 1.f)) bad = true;
         }
         if (bad) walk(true);
         const Spot s = spot_of(g, w);
@@ -214,9 +215,10 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
         for (int qb = 0; qb < 2; ++qb) {
             const int n = qb * 32 + col;
             if (n >= g.N) continue;
-            const float inv = sum[qb] == 0.f ? 0.f : 1.f / sum[qb];
-            if (lse != nullptr && hf == 0)
-                lse[((int64_t)w * g.heads + sh.hd) * g.N + n] = sum[qb] == 0.f ? -INFINITY : (top[qb] + __builtin_amdgcn_logf(exact[qb])) * kLn2;
+            const bool none = sum[qb].rounded == 0.f;
+            const float inv = none ? 0.f : 1.f / sum[qb].rounded;
+            if (LSE && hf == 0)
+                lse[((int64_t)w * g.heads + sh.hd) * g.N + n] = none ? -INFINITY : (top[qb] + __builtin_amdgcn_logf(sum[qb].exact)) * kLn2;
             bf16_t *row = out + (s.img + s.pixel(g, n)) * g.C + sh.hd * g.d;
 #pragma unroll
             for (int db = 0; db < DB; ++db) store_row<SRC>(row, O[qb][db], db, g.d, hf, inv);
@@ -435,8 +437,8 @@ inline hipError_t share_windows(const Geo &g, int *windows, int *per, int *parts
     *parts = (*windows + *per - 1) / *per;
     return hipSuccess;
 }
-template <int KX, int DB, bool SUM, int SRC>
-hipError_t launch_fwd_small(const Geo &g, const FwdArgs &a)
+template <int KX, int DB, bool SUM, bool LSE, int SRC>
+hipError_t launch_fwd_small_lse(const Geo &g, const FwdArgs &a)
 {
     Bias bi{a.bias};
     plan_scale(g, &bi);
@@ -445,12 +447,17 @@ hipError_t launch_fwd_small(const Geo &g, const FwdArgs &a)
     hipError_t e = share_windows(g, &windows, &per, &parts);
     if (e != hipSuccess) return e;
     const size_t smem = (size_t)Img<KX, 32 * DB>::STAGE * 2 + 64 + (size_t)bi.w2 * bi.w2 * 4;
-    auto kern = fwd_small_kernel<KX, DB, SUM, SRC>;
+    auto kern = fwd_small_kernel<KX, DB, SUM, LSE, SRC>;
     e = prepare_kernel((const void *)kern, nullptr);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)(parts * g.heads)), dim3(64), smem, a.st, g, bi, windows, per, a.force_max, (const bf16_t *)a.q,
                        (const bf16_t *)a.k, (const bf16_t *)a.v, (bf16_t *)a.out, a.lse);
     return hipGetLastError();
+}
+template <int KX, int DB, bool SUM, int SRC>
+hipError_t launch_fwd_small(const Geo &g, const FwdArgs &a)
+{
+    return a.lse != nullptr ? launch_fwd_small_lse<KX, DB, SUM, true, SRC>(g, a) : launch_fwd_small_lse<KX, DB, SUM, false, SRC>(g, a);
 }
 template <int K, int DB, int SRC, int SG, bool HIST>
 hipError_t launch_bwd_small_one(const Geo &g, const BwdArgs &a, Ws &ws)

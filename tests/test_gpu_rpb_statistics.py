@@ -83,3 +83,29 @@ def test_gradients_that_vanish(M, d, copies):
     centre = (2 * M - 1) ** 2 // 2
     assert abs(float(c.dbias[0, centre])) <= 1.02 * copies * off.sum()
     assert (c.dbias[0, :centre] == 0).all() and (c.dbias[0, centre + 1:] == 0).all()
+
+
+@pytest.mark.parametrize("M,d,copies", KERNELS + [(12, 46, 1), (12, 46, 100), (24, 62, 1), (5, 7, 1), (6, 64, 1), (1, 30, 1), (32, 32, 48)])
+def test_rows_of_one_key(M, d, copies):
+    """Every token sees one other alone (the one below it, and the last row of tokens none): O is that token's v and dv is dO, exactly, since
+    P is divided by itself as rounded, and is 1 in the backward; LSE is the logit, to fp32's rounding of a sum of d products and a bias
+    (d + 8 roundings of H), 2^-20 for exp2 and the logarithm, and H of it a few times."""
+    c = Case("bf16", 1, M, M, 1, d, M, 0, seed=M + d)
+    c.bias.fill_(-math.inf)
+    offset = (2 * M - 1) ** 2 // 2 - (2 * M - 1 if M > 1 else 0)
+    c.bias[:, offset] = 0.37
+    if copies > 1:
+        c = repeated(c, copies)
+    rb.rib_rpb_attn_fwd(c.p, c.q, c.k, c.v, c.bias, c.out, c.lse)
+    rb.rib_rpb_attn_bwd(c.p, c.q, c.k, c.v, c.bias, c.out, c.dout, c.lse, c.dq, c.dk, c.dv, c.dbias, c.ws)
+    down = 1 if M > 1 else 0
+    first = M - down                # rows of tokens that have a key
+    assert torch.equal(c.out[:, :first], c.v[:, down:]) and (c.out[:, first:] == 0).all()
+    assert torch.equal(c.dv[:, down:], c.dout[:, :first]) and (c.dv[:, :down] == 0).all()
+    q, k = np64(c.q)[0, :first], np64(c.k)[0, down:]
+    bias = float(np.float32(0.37))
+    want = np.full((M, M), -np.inf)
+    want[:first] = c.scale * (q * k).sum(-1) + bias
+    mag = np.zeros((M, M))
+    mag[:first] = c.scale * (abs(q) * abs(k)).sum(-1) + bias
+    close("lse", c.lse[0, 0].reshape(M, M), want, (d + 12) * H * mag + 2.0 ** -20)
