@@ -268,7 +268,8 @@ rib_status rib_features_bwd(const rib_gen_params *p, const float *W_h, const flo
  * rib_params: r must be 0, flags 0 or RIB_FLAG_FORCE_ROW_MAX, heads at most 65535 (else RIB_ERR_UNSUPPORTED); scale_p is not used.
  * Tensors may lie on boundaries of their own type (bf16: 2 bytes) and have any d of 1..64 and any token_stride; even d >= 8, even
  * strides and 4-byte boundaries are the fast case in bf16.  Everything runs on the matrix cores: bf16 storage with bf16 operands, of which P
- * and dS are rounded to nearest (logits are not: they are sums of exact products, scaled in fp32), and fp32 sums; fp32 storage in fp32. */
+ * and dS are rounded to nearest (logits are not: they are sums of exact products, scaled in fp32, whatever the scale), and fp32 sums, LSE and delta; fp32
+ * storage in fp32. */
 
 /* Forward.  bias [heads][(2M-1)^2] fp32 (from rib_rpb_table_fwd, or the caller's own); everything else as rib_window_attn_fwd. */
 rib_status rib_rpb_attn_fwd(const rib_params *p, const void *q, const void *k, const void *v, const float *bias,

@@ -9,6 +9,8 @@
 // Where all rows would not fit, the walk is cut into chunks of tiles, each with its own rows.
 #pragma once
 
+#include <cmath>
+
 #include "rib_rows.h"
 
 namespace rib {
@@ -25,7 +27,7 @@ struct Bias {
     int rows;               // bias rows in LDS at most
     int hrows;              // rows of a wave's histogram at most
     int prows;              // rows of a workgroup's sums at most
-    // Logits in the products' own unit, q.k + bias / scale: `qs` is what q is multiplied by first (1: as it is), `bs` the
+    // Logits in the products' own unit, q.k + bias / scale: `qs` is what q is multiplied by first (1: as it is; a power of two else), `bs` the
     // bias, and `c` brings a sum to base 2.  `ks`: what dS q is multiplied by.
     float qs, bs, c, ks;
     // Strips: 2^sh columns, `strip` tokens each (a multiple of 64); sh < 0: rows of the whole window.
@@ -70,15 +72,20 @@ inline void plan_order(const Geo &g, int dtype, Bias *b, bool strips)
     b->ws = 2 * b->sw - 1;
     b->inv_strip = inverse(b->strip), b->inv_ws = inverse(b->ws);
 }
-// Scales that are no ordinary positive number go into q (rounded to its type), so that neither bias / scale nor
-// an excluded pair's minus infinity comes out wrong.
+// What the products cannot carry of the scale goes into q: its sign, and a power of two where it is outside [2^-20, 2^21) (so that neither bias / scale
+// nor the sums overflow; 0 is 0 times 1).  Both leave q's digits as they are.
 inline void plan_scale(const Geo &g, Bias *b)
 {
-    const bool plain = g.scale_c >= 0x1p-40f && g.scale_c <= 0x1p40f;
-    b->qs = plain ? 1.f : g.scale_c;
-    b->bs = plain ? 1.f / g.scale_c : 1.f;
-    b->c = plain ? g.scale_c * rows::kLog2e : rows::kLog2e;
-    b->ks = plain ? g.scale_c : 1.f;
+    float rest = 1.f;
+    b->qs = 0.f;
+    if (g.scale_c != 0.f) {
+        const int e = std::ilogb(g.scale_c), k = e < -20 ? e + 20 : e > 20 ? e - 20 : 0;
+        rest = std::ldexp(std::fabs(g.scale_c), -k);
+        b->qs = std::copysign(std::ldexp(1.f, k), g.scale_c);
+    }
+    b->bs = 1.f / rest;
+    b->c = rest * rows::kLog2e;
+    b->ks = rest;
 }
 
 // The most window rows that `len` tokens from a multiple of `len` on touch.
