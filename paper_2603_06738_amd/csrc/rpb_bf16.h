@@ -343,7 +343,7 @@ struct Sums {
     float rounded, exact;
 };
 
-// One walk over the keys; `mv` holds the first tile.  MAX: with the running maximum of every row.
+// One walk over the keys; `mv` holds the first tile.  MAX: with the running maximum of every row (`top`, in the products' unit).
 template <bool MAX, int KX, int DB, bool SUM, bool LSE, int SRC, bool ALN, bool SPLIT, int W>
 __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Place &pl, const Rows &ks, const Rows &vs, bf16_t *S, float *B,
                                          const bf16x8 (&Q)[SPLIT ? 1 : 2][KX / 16], f32x16 (&O)[SPLIT ? 1 : 2][DB], Sums (&sum)[SPLIT ? 1 : 2], float (&top)[SPLIT ? 1 : 2], const Span &span,
@@ -398,19 +398,17 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
 #pragma unroll
                         for (int i = 0; i < KX / 16; ++i) s = mfma(Ak[i], Q[qb][i], s);
                         if (!ALN) mask_rows(s, key0, g.N, hf);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] *= bi.c;
                         if (MAX) {
                             float m = s[0];
 #pragma unroll
                             for (int i = 1; i < 16; ++i) m = fmaxf(m, s[i]);
                             m = fmaxf(top[qb], fmaxf(m, __shfl_xor(m, 32)));
                             // (a row of minus infinities so far: any finite stabiliser does)
-                            const float ms = m == -INFINITY ? 0.f : m, alpha = __builtin_amdgcn_exp2f(top[qb] - ms);
+                            const float ms = m == -INFINITY ? 0.f : m, alpha = __builtin_amdgcn_exp2f((top[qb] - ms) * bi.c);
                             top[qb] = m;
                             sum[qb].rounded *= alpha, sum[qb].exact *= alpha;
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) s[i] -= ms;
+                            for (int i = 0; i < 16; ++i) s[i] -= ms;            // (before the scale: the other way round a fused difference keeps the product's rounding)
 #pragma unroll
                             for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -418,7 +416,7 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
                         }
                         uint32_t P[8];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]);
+                        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * bi.c);
 #pragma unroll
                         for (int i = 0; i < 8; ++i) P[i] = pack_bf16(s[2 * i], s[2 * i + 1]);
                         if (LSE) {
@@ -460,7 +458,7 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
             float a = 1.f, b = 1.f;
             if (MAX) {
                 const float m = fmaxf(top[0], part[0]), ms = m == -INFINITY ? 0.f : m;
-                a = __builtin_amdgcn_exp2f(top[0] - ms), b = __builtin_amdgcn_exp2f(part[0] - ms);
+                a = __builtin_amdgcn_exp2f((top[0] - ms) * bi.c), b = __builtin_amdgcn_exp2f((part[0] - ms) * bi.c);
                 top[0] = m;
             }
             sum[0].rounded = sum[0].rounded * a + part[64] * b, sum[0].exact = sum[0].exact * a + part[128] * b;
@@ -540,7 +538,7 @@ __global__ __launch_bounds__(W * 64, DB == 1 ? 3 : 2) void fwd_kernel(Geo g, Bia
         const bool none = sum[qb].rounded == 0.f;
         const float inv = none ? 0.f : 1.f / sum[qb].rounded;           // (a row without a key: zeros)
         // (asked of the pointer, which is null without LSE: where `top` goes unused the compiler spills up to 181 registers)
-        if (lse != nullptr && hf == 0) lse[(int64_t)pl.u * g.N + c.index(g)] = none ? -INFINITY : (top[qb] + __builtin_amdgcn_logf(LSE ? sum[qb].exact : sum[qb].rounded)) * kLn2;
+        if (lse != nullptr && hf == 0) lse[(int64_t)pl.u * g.N + c.index(g)] = none ? -INFINITY : (top[qb] * bi.c + __builtin_amdgcn_logf(LSE ? sum[qb].exact : sum[qb].rounded)) * kLn2;
         bf16_t *row = out + (pl.img + pixel(pl.win, c)) * g.C + pl.hd * g.d;
 #pragma unroll
         for (int db = 0; db < DB; ++db) store_row<SRC>(row, O[qb][db], db, g.d, hf, inv);

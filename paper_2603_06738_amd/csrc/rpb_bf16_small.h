@@ -152,8 +152,6 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
 #pragma unroll
                     for (int i = 0; i < KX / 16; ++i) s[kb] = mfma(A[i], Q[qb][i], s[kb]);
                     if (kb == nb - 1) mask_rows(s[kb], kb * 32, g.N, hf);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[kb][i] *= bi.c;
                 }
                 top[qb] = 0.f;
                 if (max) {
@@ -176,7 +174,7 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
                     if (kb >= nb) break;
                     uint32_t P[8];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[kb][i] = __builtin_amdgcn_exp2f(s[kb][i] - top[qb]);
+                    for (int i = 0; i < 16; ++i) s[kb][i] = __builtin_amdgcn_exp2f((s[kb][i] - top[qb]) * bi.c);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) P[i] = pack_bf16(s[kb][2 * i], s[kb][2 * i + 1]);
                     if (LSE) {
@@ -218,7 +216,7 @@ __global__ __launch_bounds__(64, DB == 1 ? 3 : 2) void fwd_small_kernel(Geo g, B
             const bool none = sum[qb].rounded == 0.f;
             const float inv = none ? 0.f : 1.f / sum[qb].rounded;
             if (LSE && hf == 0)
-                lse[((int64_t)w * g.heads + sh.hd) * g.N + n] = none ? -INFINITY : (top[qb] + __builtin_amdgcn_logf(sum[qb].exact)) * kLn2;
+                lse[((int64_t)w * g.heads + sh.hd) * g.N + n] = none ? -INFINITY : (top[qb] * bi.c + __builtin_amdgcn_logf(sum[qb].exact)) * kLn2;
             bf16_t *row = out + (s.img + s.pixel(g, n)) * g.C + sh.hd * g.d;
 #pragma unroll
             for (int db = 0; db < DB; ++db) store_row<SRC>(row, O[qb][db], db, g.d, hf, inv);

@@ -201,15 +201,13 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
                     const Words16<ALN> wd = words_of<ALN>(bi, ch, (const int *)(cur + I::LT), tile, kb, hf);
                     f32x16 s = scores<DB>(cur + (kb * 32 + col) * I::STR + 4 * hf, Q, bias_block<ALN>(B + ch.c0 - mylin, wd), g.d);
                     if (!ALN) mask_rows(s, key0, g.N, hf);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] *= kLog2e;
                     if (MAX) {
                         float m = s[0];
 #pragma unroll
                         for (int i = 1; i < 16; ++i) m = fmaxf(m, s[i]);
                         m = fmaxf(top, fmaxf(m, __shfl_xor(m, 32)));
                         // (a row of minus infinities so far: any finite stabiliser does)
-                        const float ms = m == -INFINITY ? 0.f : m, alpha = __builtin_amdgcn_exp2f(top - ms);
+                        const float ms = m == -INFINITY ? 0.f : m, alpha = __builtin_amdgcn_exp2f((top - ms) * kLog2e);
                         top = m;
                         sum *= alpha;
 #pragma unroll
@@ -221,7 +219,7 @@ __device__ __forceinline__ void fwd_walk(const Geo &g, const Bias &bi, const Pla
                     }
                     float a = 0.f, b = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]);
+                    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * kLog2e);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) a += s[2 * i], b += s[2 * i + 1];
                     sum += a + b;
@@ -268,7 +266,7 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void fwd_kernel(Geo g, Bias
     if (__syncthreads_or(bad)) fwd_walk<true, DB, ALN, W>(g, bi, pl, ks, vs, S, B, Q, O, sum, top, span, cell.lin(bi), active);
     if (n >= g.N) return;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;         // (a row without a key: zeros)
-    if (lse != nullptr && hf == 0) lse[(int64_t)pl.u * g.N + cell.index(g)] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    if (lse != nullptr && hf == 0) lse[(int64_t)pl.u * g.N + cell.index(g)] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum) * kLn2;
     store_row<DB>(out + (pl.img + pixel(pl.win, cell)) * g.C + pl.hd * g.d, O, g.d, hf, inv);
 }
 

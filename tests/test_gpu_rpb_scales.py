@@ -34,3 +34,18 @@ def test_logits_are_exact(dtype, M, d, scale, qsize, ksize):
     want[:-1] = scale * (q * k).sum(-1) + bias
     mag[:-1] = abs(scale) * (abs(q) * abs(k)).sum(-1) + bias
     close("lse", c.lse[0, 0].reshape(M, M), want, (d + 13) * H * mag + 2.0 ** -20)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [1.0, 2.0 ** -39, -2.0 ** -39])
+def test_biases_next_to_the_border_do_not_exclude(dtype, scale):
+    """A bias of -9e29 for every pair: it is above -1e30, so no row is empty.  Logits of that size are all alike in fp32: O is the mean."""
+    for M in (7, 16):
+        c = Case(dtype, 1, M, M, 2, 30, M, 1, seed=M, scale=scale)
+        c.bias.fill_(-9e29)
+        rb.rib_rpb_attn_fwd(c.p, c.q, c.k, c.v, c.bias, c.out, c.lse)
+        u = 2.0 ** -8 if dtype == "bf16" else H
+        v = np64(c.v)
+        mean = v.mean((1, 2), keepdims=True)
+        close("out", c.out, np.broadcast_to(mean, v.shape), np.broadcast_to(u * abs(mean) + (M * M + 8) * H * abs(v).mean((1, 2), keepdims=True), v.shape))
+        close("lse", c.lse, np.full(c.lse.shape, float(np.float32(-9e29))), np.full(c.lse.shape, 8 * H * 9e29))
