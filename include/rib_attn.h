@@ -262,7 +262,9 @@ rib_status rib_features_bwd(const rib_gen_params *p, const float *W_h, const flo
  *
  * EXCLUDED PAIRS.  A bias of minus infinity, or any at or below -1e30 (so also the lowest value of a type), excludes the pairs of its
  * offset: their probability and their gradients are exactly zero.  A row whose pairs are all excluded gives O = 0,
- * LSE = minus infinity and adds nothing to any gradient.  (An infinity or NaN in q, k, v or d_out may spread over its
+ * LSE = minus infinity and adds nothing to any gradient.  Biases above that are ordinary numbers, and logits are fp32: a row whose logits all lie
+ * near X keeps 2^-24 |X| of their differences, and its probabilities in the backward are off by up to 2^-20 |X|, but never above 1.  So a mask that may
+ * cover whole rows is better given as minus infinity than as -1e9.  (An infinity or NaN in q, k, v or d_out may spread over its
  * own (window, head), excluded pairs too, and through the sum over windows into dbias.)
  *
  * rib_params: r must be 0, flags 0 or RIB_FLAG_FORCE_ROW_MAX, heads at most 65535 (else RIB_ERR_UNSUPPORTED); scale_p is not used.

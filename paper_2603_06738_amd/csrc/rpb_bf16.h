@@ -685,7 +685,7 @@ __global__ __launch_bounds__(W * 64, DB == 2 && K == 64 && ALN && !SPLIT ? 1 : 2
                         for (int i = 0; i < K / 16; ++i) p = mfma(Av[i], D[qb][i], p);
                         if (!ALN) mask_rows(s, key0, g.N, hf);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], bi.c, -mylse[qb])) * (MINUS ? p[i] : p[i] - mydelta[qb]);
+                        for (int i = 0; i < 16; ++i) s[i] = prob(fmaf(s[i], bi.c, -mylse[qb])) * (MINUS ? p[i] : p[i] - mydelta[qb]);
                         if (HIST && CARRY && qb == 1) add_offsets<ALN>(mine - mylin[QB - 1], wd, s + held);
                         else if (HIST && CARRY) held = s;
                         else if (HIST && (ALN || n0 + (sel + qb) * 32 + col < g.N)) add_offsets<ALN>(mine - mylin[qb], wd, s);     // (many lanes at one word are slow)
@@ -831,7 +831,7 @@ __global__ __launch_bounds__(W * 64, DB == 1 || SPLIT ? 2 : 1) void dkv_kernel(G
                         for (int i = 0; i < K / 16; ++i) p = mfma(Ad[i], Vb[b][i], p);
                         uint32_t P[8], G[8];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], bi.c, ((const float *)&l[i >> 2])[i & 3]));
+                        for (int i = 0; i < 16; ++i) s[i] = prob(fmaf(s[i], bi.c, ((const float *)&l[i >> 2])[i & 3]));
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             P[i] = pack_bf16(s[2 * i], s[2 * i + 1]);

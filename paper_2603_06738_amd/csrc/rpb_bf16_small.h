@@ -337,7 +337,7 @@ __global__ __launch_bounds__(64, DB == 1 ? 2 : 1) void bwd_small_kernel(Geo g, B
                 for (int i = 0; i < K / 16; ++i) p = mfma(Av[i], Db[qb][i], p);
                 if (kb == nb - 1) mask_rows(s, kb * 32, g.N, hf);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], bi.c, mylse)) * (p[i] + mydelta);
+                for (int i = 0; i < 16; ++i) s[i] = prob(fmaf(s[i], bi.c, mylse)) * (p[i] + mydelta);
                 if (HIST && qb * 32 + col < g.N) add_offsets<false>(H + ch.c0 - mylin[qb], at, s);      // (many lanes at one word are slow)
                 uint32_t P[8];
 #pragma unroll
@@ -390,7 +390,7 @@ __global__ __launch_bounds__(64, DB == 1 ? 2 : 1) void bwd_small_kernel(Geo g, B
                 for (int i = 0; i < K / 16; ++i) p = mfma(Ad[i], Vb[kb][i], p);
                 uint32_t P[8], G[8];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], bi.c, ((const float *)&e[i >> 2])[i & 3]));
+                for (int i = 0; i < 16; ++i) s[i] = prob(fmaf(s[i], bi.c, ((const float *)&e[i >> 2])[i & 3]));
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     P[i] = pack_bf16(s[2 * i], s[2 * i + 1]);

@@ -97,6 +97,10 @@ inline int most_rows(int len, const Geo &g, const Bias &b)
     return rows < g.M ? rows : g.M;
 }
 
+// A probability made again from LSE, 2^x: at most 1.  (A row whose logits all lie near -1e9, say, has an LSE that fp32 rounds by tens; without the bound,
+// which is a bit of the instruction, such a row's gradients would overflow and take its window's with them.)
+__device__ __forceinline__ float prob(float x) { return __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(x), 0.f, 1.f); }
+
 __device__ __forceinline__ int row_of(int n, uint32_t inv_m) { return (int)__umulhi((uint32_t)n, inv_m); }
 // The n-th token of the walk: its row and column.
 struct Cell {

@@ -347,7 +347,7 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dq_kernel(Geo g, Bias 
                     const f32x16 p = scores<DB>(row + I::YR, D, z, g.d);
                     if (!ALN) mask_rows(s, key0, g.N, hf);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f((s[i] - L) * kLog2e) * (p[i] - delta);
+                    for (int i = 0; i < 16; ++i) s[i] = prob((s[i] - L) * kLog2e) * (p[i] - delta);
                     if (HIST && (ALN || n < g.N)) {         // (many lanes at one word are slow)
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
@@ -432,7 +432,7 @@ __global__ __launch_bounds__(W * 64, W == 1 ? 1 : 2) void dkv_kernel(Geo g, Bias
                         const float lr[4] = {l.x, l.y, l.z, l.w}, dr[4] = {dl.x, dl.y, dl.z, dl.w};
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
-                            s[4 * a + r] = __builtin_amdgcn_exp2f((s[4 * a + r] + lr[r]) * kLog2e);
+                            s[4 * a + r] = prob((s[4 * a + r] + lr[r]) * kLog2e);
                             p[4 * a + r] = (p[4 * a + r] + dr[r]) * s[4 * a + r];
                         }
                     }
