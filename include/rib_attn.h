@@ -277,8 +277,9 @@ rib_status rib_features_bwd(const rib_gen_params *p, const float *W_h, const flo
 rib_status rib_rpb_attn_fwd(const rib_params *p, const void *q, const void *k, const void *v, const float *bias,
                             void *out, float *lse, void *stream);
 
-/* Bytes of device scratch the backward needs (0 if the parameters are invalid): 8 a (token, head), and
- * partial sums of dbias of every 64 to 256 tokens of a window and head. */
+/* Bytes of device scratch the backward needs (0 if the parameters are invalid): 8 a (token, head), rounded up to a multiple of 256, and
+ * partial sums of dbias of every 64 to 256 tokens of a window and head.  The sums of a window grow with the fourth power of its side: one of 6 heads takes
+ * 16 MiB at side 96 in bf16, 780 at 256.  Without dbias (NULL) the first part is enough: 8 * B * H * W * heads, rounded up. */
 size_t rib_rpb_attn_bwd_workspace_bytes(const rib_params *p);
 
 /* Backward: the probabilities are made again from q, k, bias and lse,

@@ -43,7 +43,8 @@ rib_status run_bwd(const rib_params *p, const void *q, const void *k, const void
     if ((!packed && (!q || !k || !v)) || !bias || !out || !d_out || !lse || !dq || !dk || !dv) return RIB_ERR_NULL;
     if (!aligned({q, k, v, out, d_out, dq, dk, dv}, value_bytes(p->dtype)) || !aligned({bias, lse, dbias}, 4) || !aligned({ckpt}, 16))
         return RIB_ERR_SHAPE;
-    if (!workspace || !aligned({workspace}, 256) || workspace_bytes < ws_layout(g, p->dtype).total) return RIB_ERR_WORKSPACE;
+    const Ws ws = ws_layout(g, p->dtype);
+    if (!workspace || !aligned({workspace}, 256) || workspace_bytes < (dbias != nullptr ? ws.total : ws.part)) return RIB_ERR_WORKSPACE;
     const BwdArgs a{q, k, v, (const uint8_t *)ckpt, bias, out, d_out, lse, dq, dk, dv, dbias, workspace, (hipStream_t)stream};
     return status_of(p->dtype == RIB_BF16 ? launch_bwd_bf16(g, a) : launch_bwd_f32(g, a));
 }
