@@ -310,7 +310,7 @@ rib_status rib_rpb_table_fwd(const rib_rpb_params *p, const void *table, const i
 
 /* dtable[head][b] = sum of dbias[head][o] over the offsets with index[o] == b (zero for a bucket without one); OVERWRITTEN.
  * dbias is what rib_rpb_attn_bwd returns, possibly summed over layers that share the table.  Sums do not depend on the order of their
- * terms (run-to-run identical results). */
+ * terms (run-to-run identical results); every term counts to 2^-44 of its bucket's largest. */
 rib_status rib_rpb_table_bwd(const rib_rpb_params *p, const float *dbias, const int32_t *index, void *dtable, void *stream);
 
 /* ------------------------------------------------------------------------

@@ -25,8 +25,8 @@ __global__ __launch_bounds__(256) void table_fwd_kernel(int L, int buckets, cons
 // dtable[head][b] = sum of dbias[head][o] over the offsets of bucket b.
 //
 // Many offsets share a bucket, so their values are added in LDS, as 64-bit whole numbers: such sums do not depend on the order of
-// the additions.  The unit is the largest value of the head over 2^(62 - bits of the number of offsets), so sums cannot overflow and a
-// bucket whose gradient is 2^-21 of the largest still has 24 bits.  Values that are not finite are noted by kind beside the sums.
+// the additions.  A bucket's unit is the power of two above its largest value over 2^(62 - bits of the number of offsets): sums cannot overflow, and
+// a term is off by 2^-44 of its bucket's largest at most (256 x 256 windows: 18 bits).  Values that are not finite are noted by kind beside the sums.
 constexpr int kBuckets = 2048;          // buckets a workgroup at most
 // Every workgroup of a head reads all offsets and adds those of its `chunk` buckets: the conversions, not the reads, are what costs
 // (36481 offsets in 625 buckets, us: 36 in one workgroup a head, 15 in 16).
@@ -35,44 +35,43 @@ __global__ __launch_bounds__(1024) void table_bwd_kernel(int L, int buckets, int
                                                          const int32_t *__restrict__ index, T *__restrict__ dtable)
 {
     __shared__ unsigned long long sum[kBuckets];
-    __shared__ uint32_t odd[kBuckets];
-    __shared__ uint32_t top;
+    __shared__ uint32_t odd[kBuckets], top[kBuckets];
     const int hd = blockIdx.y, b0 = blockIdx.x * chunk, tid = threadIdx.x;
     const float *x = dbias + (int64_t)hd * L;
-    if (tid == 0) top = 0u;
-    for (int i = tid; i < chunk; i += 1024) sum[i] = 0ull, odd[i] = 0u;
+    for (int i = tid; i < chunk; i += 1024) sum[i] = 0ull, odd[i] = top[i] = 0u;
     __syncthreads();
-    uint32_t m = 0u;
-#pragma unroll 8
-    for (int o = tid; o < L; o += 1024) {
-        const uint32_t a = __float_as_uint(x[o]) & 0x7fffffffu;
-        if (a < 0x7f800000u && a > m) m = a;
-    }
-    atomicMax(&top, m);
+    // f(bucket of this workgroup, value) for all offsets (eight loads in flight)
+    auto each = [&](auto f) {
+        for (int o0 = tid; o0 < L; o0 += 8 * 1024) {
+            int at[8];
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int o = o0 + j * 1024 < L ? o0 + j * 1024 : L - 1;
+                at[j] = o0 + j * 1024 < L ? index[o] : -1, v[j] = x[o];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int i = at[j] - b0;
+                if ((uint32_t)at[j] < (uint32_t)buckets && (uint32_t)i < (uint32_t)chunk) f(i, v[j]);
+            }
+        }
+    };
+    each([&](int i, float v) {
+        const uint32_t a = __float_as_uint(v) & 0x7fffffffu;
+        if (a >= 0x7f800000u) atomicOr(&odd[i], v != v ? 4u : v > 0.f ? 1u : 2u);
+        else atomicMax(&top[i], a);
+    });
     __syncthreads();
-    int e;
-    frexp((double)__uint_as_float(top), &e);            // the largest is below 2^e
-    const double unit = ldexp(1., e + bits - 62);
-    const double per = ldexp(1., 62 - bits - e);
-    for (int o0 = tid; o0 < L; o0 += 8 * 1024) {           // (eight loads in flight)
-        int at[8];
-        float v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int o = o0 + j * 1024 < L ? o0 + j * 1024 : L - 1;
-            at[j] = o0 + j * 1024 < L ? index[o] : -1, v[j] = x[o];
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int i = at[j] - b0;
-            if ((uint32_t)at[j] >= (uint32_t)buckets || (uint32_t)i >= (uint32_t)chunk) continue;
-            if ((__float_as_uint(v[j]) & 0x7f800000u) == 0x7f800000u) atomicOr(&odd[i], v[j] != v[j] ? 4u : v[j] > 0.f ? 1u : 2u);
-            else atomicAdd(&sum[i], (unsigned long long)llrint((double)v[j] * per));
-        }
-    }
+    // 2^k of a bucket's unit: its largest is below 2^(k + 62 - bits)
+    auto unit = [&](int i) { return (int)(top[i] >> 23 > 0u ? top[i] >> 23 : 1u) - 126 + bits - 62; };
+    auto power = [](int k) { return __longlong_as_double((long long)(1023 + k) << 52); };
+    each([&](int i, float v) {
+        if ((__float_as_uint(v) & 0x7f800000u) != 0x7f800000u) atomicAdd(&sum[i], (unsigned long long)llrint((double)v * power(-unit(i))));
+    });
     __syncthreads();
     for (int i = tid; i < chunk && b0 + i < buckets; i += 1024) {
-        float v = (float)((double)(long long)sum[i] * unit);
+        float v = (float)((double)(long long)sum[i] * power(unit(i)));
         if (odd[i] != 0u) v = odd[i] == 1u ? INFINITY : odd[i] == 2u ? -INFINITY : NAN;
         store_as(dtable + (int64_t)hd * buckets + b0 + i, v);
     }
