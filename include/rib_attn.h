@@ -260,6 +260,9 @@ rib_status rib_features_bwd(const rib_gen_params *p, const float *W_h, const flo
  *     offset(i, j) = (iy(i) - iy(j) + M-1) * (2M-1) + ix(i) - ix(j) + M-1         (query minus key, row-major)
  *     P = softmax over j of S,   O[i] = sum_j P[i][j] v[j],   LSE[i] = log sum_j exp(S[i][j])
  *
+ * SHIFTED WINDOWS.  Pixels that wrap around attend freely, as with the implicit bias, and the bias knows the offset alone.  Layers trained with a mask between
+ * the regions that a shift brings together, as shifted-window transformers commonly are, give other results here wherever shift > 0.
+ *
  * EXCLUDED PAIRS.  A bias of minus infinity, or any at or below -1e30 (so also the lowest value of a type), excludes the pairs of its
  * offset: their probability and their gradients are exactly zero.  A row whose pairs are all excluded gives O = 0,
  * LSE = minus infinity and adds nothing to any gradient.  Biases above that are ordinary numbers, and logits are fp32: a row whose logits all lie
@@ -333,8 +336,9 @@ rib_status rib_checkpoint_pack(const rib_params *p, const void *q, const void *k
 /* The values a checkpoint stands for, as tensors of p->dtype: for rib_window_attn_bwd and the gated backward, or any other use. */
 rib_status rib_checkpoint_unpack(const rib_params *p, const void *ckpt, void *q, void *k, void *v, void *stream);
 
-/* rib_rpb_attn_bwd with the values that `ckpt` stands for in place of q, k and v (bit for bit what it gives for those as tensors),
- * read from the checkpoint by the kernels themselves.  out and lse are those of the forward, on the values as they were. */
+/* rib_rpb_attn_bwd with the values that `ckpt` stands for in place of q, k and v, read from the checkpoint by the kernels themselves: bit for
+ * bit what it gives for those as tensors, where these lie as well as out, d_out and the gradients do (in bf16 tensors and strides that miss the fast case
+ * above run on kernels that add in another order; a checkpoint never does so by itself).  out and lse are those of the forward, on the values as they were. */
 rib_status rib_rpb_attn_bwd_ckpt(const rib_params *p, const void *ckpt, const float *bias, const void *out, const void *d_out,
                                  const float *lse, void *dq, void *dk, void *dv, float *dbias,
                                  void *workspace, size_t workspace_bytes, void *stream);

@@ -11,15 +11,14 @@
 // instructions a block, and cost as much accuracy as the rounding of P (2-norm errors of a training step 2.5e-3 so, 3.4e-3 with it; forward 8 %,
 // whole step 5 % slower).
 //
-// LSE and delta stay in fp32: per row beside the lane's own in dq, in LDS beside the streamed rows in dkv, where -delta is the C operand of dP's
-// product.  (As bf16 pairs in two more columns of the rows they cost nothing in 30 columns and a third of a row's in 32, and lose 2^-17 of LSE, which is
-// an exponent.)
+// LSE and delta stay in fp32: the lane's own in dq, in LDS beside the streamed rows in dkv, where -delta is the C operand of dP's product.  (As
+// bf16 pairs in two more columns of the rows they were 4 % of dkv cheaper up to 30 channels and dearer from 32 on, and lost 2^-17 of LSE, which is an exponent.)
 //
-// What bounds it, by counters (16 images of 96 x 96, 32 x 32 windows, 6 heads of 30; forward / dq / dkv 194 / 394 / 315 us): the vector issue is
-// busy 60 % of the time and the matrix pipe 29 / 20 / 35 %, and the two hardly overlap.  A block of the forward has 60 vector instructions,
-// 40 of them exp2, scale and pack.  Parts taken out, us: staging -20 / -32 / -39, the barriers too -22 / -43 / -46, the bias -18 / -17 / -14.  Three
-// waves a SIMD (168 registers) in the forward up to 32 channels, two elsewhere.  Tiles of 128 tokens (half the barriers): forward the same, dq 5 %
-// slower.
+// What bounds it, by counters (16 images of 96 x 96, 32 x 32 windows, 6 heads of 30; forward with LSE / dq / dkv 207 / 374 / 312 us, forward without
+// LSE 188): the vector issue is busy 81 / 57 / 60 % of the time and the matrix pipe 26 / 21 / 35 %, and the two hardly overlap.  A block of the forward has 60
+// vector instructions in its loop, 40 of them exp2, scale and pack, and 17 more with LSE.  Parts taken out (of kernels without LSE's sum, with the pairs), us: staging -20 /
+// -32 / -39, the barriers too -22 / -43 / -46, the bias -18 / -17 / -14.  Three waves a SIMD (168 registers) in the forward up to 32 channels, two
+// elsewhere, one in the backward of wide heads (below).  Tiles of 128 tokens (half the barriers): forward the same, dq 5 % slower.
 #pragma once
 
 #include "rpb_common.h"

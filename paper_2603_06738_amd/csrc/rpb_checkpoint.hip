@@ -4,7 +4,8 @@
 // the smallest for which the row's largest fits 127 steps (248 at most: above 127 * 2^121 codes stay at 127).  Codes lie in the units' own token order, so what the backward
 // reads of a unit is contiguous.  Codes under a power of two are exact in either storage type.
 // Bound by memory: q, k, v read once and a little over half of that (bf16; a quarter, fp32) written.  16 images of 96 x 96, 6 heads of 30, bf16:
-// 76 us, 247 MB, 3.2 TB/s of the 5.1 a copy reaches (a head at a time, rows in 16 lanes 256 us, in 4 lanes 90).
+// pack 78 us, 247 MB, 3.2 TB/s of the 5.1 a copy reaches (a head at a time, rows in 16 lanes 256 us, in 4 lanes 90); unpack 100 us: it stores value by value,
+// and is for users of other backward passes, since the one here reads codes.
 #include "rpb_common.h"
 
 namespace rib {

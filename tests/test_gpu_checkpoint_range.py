@@ -102,3 +102,33 @@ def test_reference_agrees_below_the_top():
     codes, exps = ref.pack(x, 1, 4, 0)
     mine = expected(x.reshape(16, 10))
     assert np.array_equal(codes[0, :, :10], mine[0]) and np.array_equal(exps[0], mine[1])
+
+
+@pytest.mark.parametrize("M,d", [(7, 30), (16, 30), (20, 32), (16, 64)])
+def test_backward_from_a_checkpoint_beside_unaligned_tensors(M, d):
+    """out, d_out and the gradients one value into their allocations: as from the unpacked tensors, which then run on the same kernels however they
+    lie.  Where out, d_out and the gradients are aligned and the unpacked tensors are not, the bits may differ: only the roundings do (three of
+    bf16's on the way of any term: P or dS, the sum's order, the output)."""
+    c = Case("bf16", 1, M, 2 * M, 1, d, M, 1, seed=M)
+    c.forward()
+    ck = packed(c)
+    held = [torch.empty_like(c.q) for _ in range(3)]
+    rb.rib_checkpoint_unpack(c.p, ck, *held)
+    names = ("out", "dout", "dq", "dk", "dv")
+
+    def off(x):
+        view = torch.full((x.numel() + 8,), 7.0, dtype=x.dtype, device=DEV)[1:1 + x.numel()].view(x.shape)
+        return view.copy_(x)
+
+    def run(call, *first, t):
+        call(c.p, *first, c.bias, t["out"], t["dout"], c.lse, t["dq"], t["dk"], t["dv"], c.dbias, c.ws)
+        return [t[n].clone() for n in ("dq", "dk", "dv")] + [c.dbias.clone()]
+
+    aligned = {n: getattr(c, n) for n in names}
+    moved = {n: off(x) for n, x in aligned.items()}
+    want = run(rb.rib_rpb_attn_bwd_ckpt, ck, t=moved)
+    for tensors in (held, [off(x) for x in held]):
+        for a, b in zip(want, run(rb.rib_rpb_attn_bwd, *tensors, t=moved)):
+            assert torch.equal(a, b)
+    for a, b in zip(run(rb.rib_rpb_attn_bwd_ckpt, ck, t=aligned), run(rb.rib_rpb_attn_bwd, *[off(x) for x in held], t=aligned)):
+        assert (a - b).float().norm() <= 3 * 2.0 ** -8 * a.float().norm()
