@@ -333,7 +333,7 @@ __device__ __forceinline__ void join(f32x16 (&v)[DB], float *lds, bool odd)
 // Two denominators of a row.  O's weights are P as rounded, so O is divided by the sum of those: a row of one key gives its v.  LSE wants P before it is rounded (with
 // few keys the other sum would move it by up to 2^-8).  The first is a column of ones in V where V's block has one to spare, else (SUM)
 // one instruction for two values of P; the second 16 additions a block, made only where LSE is asked for (forward of 32 x 32 windows, 6 heads of 30,
-// 16 images: 191 us without, 210 with).
+// 16 images: 188 us without, 207 with).
 __device__ __forceinline__ float add_pair(float sum, uint32_t pair)
 {
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3f803f80u), sum, false);

@@ -27,7 +27,7 @@ struct Bias {
     int rows;               // bias rows in LDS at most
     int hrows;              // rows of a wave's histogram at most
     int prows;              // rows of a workgroup's sums at most
-    // Logits in the products' own unit, q.k + bias / scale: `qs` is what q is multiplied by first (1: as it is; a power of two else), `bs` the
+    // Logits in the products' own unit, q.k + bias / scale: `qs` is what q is multiplied by first (1: as it is; -1, 0 or a power of two else), `bs` the
     // bias, and `c` brings a sum to base 2.  `ks`: what dS q is multiplied by.
     float qs, bs, c, ks;
     // Strips: 2^sh columns, `strip` tokens each (a multiple of 64); sh < 0: rows of the whole window.
